@@ -357,6 +357,99 @@ int mfpsn_backward_time_last(const mfpsn_desc* desc, const void* x, const void* 
  * MFPSN_ERR_ALIGN; count = 0 does nothing. */
 int mfpsn_spikes_to_input(const uint8_t* spikes, int64_t count, int32_t dtype, void* x, void* stream);
 
+/* Layer norm over the channels, the normalisation that depends on no batch
+ * and no later time step (a step-by-step layer has neither):
+ *   mu = mean_c x,  var = mean_c (x - mu)^2,  rstd = 1/sqrt(var + eps)
+ *   y[m,c,s] = gamma[c] * (x[m,c,s] - mu[m,s]) * rstd[m,s] + beta[c]
+ *   x, y, grad_y, grad_x : [M][C][S] storage type (MFPSN_F32, MFPSN_BF16;
+ *            arithmetic in float, rounded once).  A time-first tensor
+ *            [T][N][C][S] has M = T*N; a time-last one [N][C][S][T] has M = N
+ *            and its S and T as one S.
+ *   gamma, beta : float [C], either may be NULL (1 and 0)
+ *   mean, rstd  : float [M][S], written by the forward where not NULL (both or
+ *            neither), read by the backward
+ * mfpsn_layer_norm_backward, with xh = (x - mu) rstd and a = gamma grad_y:
+ *   grad_x = rstd (a - mean_c a - xh mean_c(a xh)),
+ *   grad_gamma = sum_{m,s} grad_y xh,  grad_beta = sum_{m,s} grad_y
+ *   grad_gamma, grad_beta : float [C], either may be NULL.  Their sums are
+ *            added in a fixed order: repeated calls give the same bits.
+ *   workspace : >= mfpsn_layer_norm_workspace_size bytes, 4-byte aligned
+ *            (needed where grad_gamma or grad_beta is given; contents ignored)
+ * Outputs must not overlap inputs.  M, C, S >= 0, M*C*S < 2^60 (else
+ * MFPSN_ERR_SHAPE); eps >= 0 and finite (else MFPSN_ERR_PARAM).  Tensors are
+ * aligned to their element size. */
+int mfpsn_layer_norm_forward(int64_t M, int32_t C, int32_t S, int32_t dtype, const void* x, const float* gamma,
+                             const float* beta, float eps, void* y, float* mean, float* rstd, void* stream);
+int mfpsn_layer_norm_workspace_size(int64_t M, int32_t C, int32_t S, size_t* bytes);
+int mfpsn_layer_norm_backward(int64_t M, int32_t C, int32_t S, int32_t dtype, const void* x, const float* gamma,
+                              const float* mean, const float* rstd, const void* grad_y, void* grad_x,
+                              float* grad_gamma, float* grad_beta, void* workspace, size_t workspace_bytes,
+                              void* stream);
+
+/* Gated delta rule: a memory over the whole past beside the neuron's finite
+ * receptive field, with a whole-sequence form (forward and backward) and a
+ * step-by-step form like the neuron's.  Per sequence n and value head h, with
+ * the key head h / (Hv/Hk):
+ *   S_t = e^{g_t} S_{t-1} + beta_t k_t (v_t - e^{g_t} S_{t-1}^T k_t)^T
+ *   o_t = scale * S_t^T q_t                            (S: [Dk][Dv])
+ * Layouts, time-first, storage type MFPSN_F32 or MFPSN_BF16 unless noted:
+ *   q, k : [T][N][Hk][Dk];  v, o : [T][N][Hv][Dv].  Rows (t, n) of q, k and v
+ *          lie q_row, k_row, v_row elements apart (0: dense), so that slices of
+ *          one projection's output are taken as they are; all else is dense
+ *   g    : [T][N][Hv] log of the decay, normally <= 0; -inf forgets everything
+ *   beta : [T][N][Hv] write strength
+ *   lengths   : int32 [N] or NULL (T for all); clamped into [0, T].  Steps
+ *          t >= lengths[n] are not read, leave the state as it is, and get zeros
+ *          in o and in every gradient
+ *   state_in  : float [N][Hv][Dk][Dv] or NULL (zeros)
+ *   state_out : float [N][Hv][Dk][Dv] or NULL; may be state_in
+ * The rule is stable for beta |k|^2 <= 2 (unit keys, beta in [0, 1]).
+ * Arithmetic: the state is float; MFPSN_F32 products are float, MFPSN_BF16 ones
+ * are 16-bit matrix products summed in float, of which those that make the next
+ * state take their operands as sums of two 16-bit numbers (the state is as
+ * exact as float products make it), the others round them once.  A value that is
+ * not finite spoils its own and the later outputs of its sequence and head and,
+ * in the whole-sequence form, those of the 64 steps around it (a chunk).
+ *
+ * mfpsn_delta_forward: `saved` (mfpsn_delta_saved_size bytes, 16-byte aligned,
+ * or NULL) keeps what the backward needs.  Without it the call needs
+ * mfpsn_delta_workspace_size bytes of `workspace` (16-byte aligned; NULL and 0
+ * where that is 0), with it none.
+ * mfpsn_delta_backward, of the same inputs, from the forward's saved:
+ *   grad_o : [T][N][Hv][Dv] storage type;  grad_state_out : float like
+ *            state_out, the gradient of it, or NULL (zeros)
+ *   grad_q, grad_k, grad_v, grad_g, grad_beta : dense, storage type; q's and k's
+ *            are summed over the value heads that share them
+ *   grad_state_in : float like state_in, or NULL
+ *   workspace : >= mfpsn_delta_backward_workspace_size bytes, 16-byte aligned
+ * mfpsn_delta_step: one time step for every sequence (desc->T is ignored): q, k
+ * [N][Hk][Dk], v, o [N][Hv][Dv], g, beta [N][Hv], state_out may be state_in.
+ * Contents of workspaces are ignored on entry; calls that may overlap need
+ * workspaces of their own.  No sum's order depends on timing: repeated calls
+ * give the same bits. */
+typedef struct mfpsn_delta_desc {
+    int32_t T, N;    /* steps, sequences, each >= 0                                */
+    int32_t Hk, Hv;  /* key and value heads, Hk >= 1, Hv a multiple of Hk          */
+    int32_t Dk, Dv;  /* 1..128, 1..256                                             */
+    int32_t dtype;   /* MFPSN_F32, MFPSN_BF16                                      */
+    float scale;     /* of the outputs, finite                                     */
+    int64_t q_row, k_row, v_row; /* 0, or at least a row's Hk*Dk (Hv*Dv), < 2^40   */
+} mfpsn_delta_desc;
+
+int mfpsn_delta_workspace_size(const mfpsn_delta_desc* desc, size_t* bytes);
+int mfpsn_delta_saved_size(const mfpsn_delta_desc* desc, size_t* bytes);
+int mfpsn_delta_backward_workspace_size(const mfpsn_delta_desc* desc, size_t* bytes);
+int mfpsn_delta_forward(const mfpsn_delta_desc* desc, const void* q, const void* k, const void* v, const void* g,
+                        const void* beta, const int32_t* lengths, const float* state_in, void* o, float* state_out,
+                        void* saved, size_t saved_bytes, void* workspace, size_t workspace_bytes, void* stream);
+int mfpsn_delta_backward(const mfpsn_delta_desc* desc, const void* q, const void* k, const void* v, const void* g,
+                         const void* beta, const int32_t* lengths, const void* saved, size_t saved_bytes,
+                         const void* grad_o, const float* grad_state_out, void* grad_q, void* grad_k, void* grad_v,
+                         void* grad_g, void* grad_beta, float* grad_state_in, void* workspace,
+                         size_t workspace_bytes, void* stream);
+int mfpsn_delta_step(const mfpsn_delta_desc* desc, const void* q, const void* k, const void* v, const void* g,
+                     const void* beta, const float* state_in, void* o, float* state_out, void* stream);
+
 /* MFPSN_ABI_VERSION of the loaded library. */
 int32_t mfpsn_abi_version(void);
 

@@ -93,6 +93,16 @@ def _units():
     obj = os.path.join(BUILD, "stream.o")
     units.append((obj, [HIPCC, *DEVICE_FLAGS, f"-I{INCLUDE}", f"-I{CSRC}", "-c", stream_src, "-o", obj],
                   [stream_src, os.path.join(CSRC, "mfpsn_stream.h"), *api_headers]))
+    norm_src = os.path.join(CSRC, "mfpsn_norm.hip")
+    obj = os.path.join(BUILD, "norm.o")
+    units.append((obj, [HIPCC, *DEVICE_FLAGS, f"-I{INCLUDE}", f"-I{CSRC}", "-c", norm_src, "-o", obj],
+                  [norm_src, os.path.join(CSRC, "mfpsn_norm.h"), os.path.join(CSRC, "mfpsn_internal.h")]))
+    for name in ("mfpsn_delta", "mfpsn_delta_step"):
+        delta_src = os.path.join(CSRC, name + ".hip")
+        obj = os.path.join(BUILD, name[6:] + ".o")
+        units.append((obj, [HIPCC, *DEVICE_FLAGS, f"-I{INCLUDE}", f"-I{CSRC}", "-c", delta_src, "-o", obj],
+                      [delta_src, os.path.join(CSRC, "mfpsn_delta.h"), os.path.join(CSRC, "mfpsn_delta_mat.h"),
+                       os.path.join(CSRC, "mfpsn_internal.h")]))
     na_src = os.path.join(CSRC, "mfpsn_noalloc.hip")
     obj = os.path.join(BUILD, "noalloc.o")
     units.append((obj, [HIPCC, *DEVICE_FLAGS, f"-I{INCLUDE}", f"-I{CSRC}", "-c", na_src, "-o", obj],
@@ -100,14 +110,15 @@ def _units():
     obj = os.path.join(BUILD, "kernels_misc.o")
     units.append((obj, [HIPCC, *DEVICE_FLAGS, f"-I{INCLUDE}", f"-I{CSRC}", "-DMFPSN_TU_MISC",
                         "-c", src, "-o", obj], [src, *headers]))
-    for name in ("mfpsn_api.cpp", "mfpsn_api_ext.cpp", "mfpsn_dispatch.cpp"):
+    for name in ("mfpsn_api.cpp", "mfpsn_api_ext.cpp", "mfpsn_api_seq.cpp", "mfpsn_dispatch.cpp"):
         obj = os.path.join(BUILD, name.replace(".cpp", ".o"))
         cpp = os.path.join(CSRC, name)
         units.append((obj, ["g++", *HOST_FLAGS, f"-I{INCLUDE}", f"-I{CSRC}", "-c", cpp, "-o", obj],
                       [cpp, os.path.join(CSRC, "mfpsn_stream.h"), os.path.join(CSRC, "mfpsn_qgrad.h"),
                        os.path.join(CSRC, "mfpsn_bn.h"), os.path.join(CSRC, "mfpsn_validate.h"),
                        os.path.join(CSRC, "mfpsn_chain.h"), os.path.join(CSRC, "mfpsn_tl.h"),
-                       os.path.join(CSRC, "mfpsn_tl_tile.h"), *api_headers]))
+                       os.path.join(CSRC, "mfpsn_tl_tile.h"), os.path.join(CSRC, "mfpsn_norm.h"),
+                       os.path.join(CSRC, "mfpsn_delta.h"), *api_headers]))
     return units
 
 

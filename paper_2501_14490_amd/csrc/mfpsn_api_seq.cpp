@@ -1,0 +1,348 @@
+// C ABI of libmfpsn.so: the sequence operators beside the neuron (layer norm,
+// gated delta rule).  Declarations and the contract of every entry point are
+// in include/mfpsn.h.
+#include "mfpsn.h"
+
+#include <math.h>
+#include <stdint.h>
+
+#include "mfpsn_delta.h"
+#include "mfpsn_norm.h"
+#include "mfpsn_validate.h"
+
+using namespace mfpsn;
+
+namespace {
+
+int validate_norm(int64_t M, int32_t C, int32_t S)
+{
+    if (M < 0 || C < 0 || S < 0)
+        return MFPSN_ERR_SHAPE;
+    const int64_t cs = (int64_t)C * S;
+    if (cs > 0 && M > (((int64_t)1 << 60) - 1) / cs)
+        return MFPSN_ERR_SHAPE;
+    if (C > 0 && S > 0 && M > ((int64_t)1 << 60) / S)
+        return MFPSN_ERR_SHAPE;
+    return MFPSN_OK;
+}
+
+bool float_dtype(int32_t dtype) { return dtype == MFPSN_F32 || dtype == MFPSN_BF16; }
+
+// What a call of the delta rule does not read or write is not asked for
+int validate_delta(const mfpsn_delta_desc* d)
+{
+    if (!d)
+        return MFPSN_ERR_NULL;
+    if (!float_dtype(d->dtype))
+        return MFPSN_ERR_DTYPE;
+    if (d->T < 0 || d->N < 0 || d->Hk < 1 || d->Hv < 1 || d->Hv % d->Hk != 0 || d->Dk < 1 || d->Dk > kDeltaMaxDk ||
+        d->Dv < 1 || d->Dv > kDeltaMaxDv)
+        return MFPSN_ERR_SHAPE;
+    const int64_t qk = (int64_t)d->Hk * d->Dk, v = (int64_t)d->Hv * d->Dv, most = (int64_t)1 << 40;
+    if ((d->q_row != 0 && (d->q_row < qk || d->q_row >= most)) || (d->k_row != 0 && (d->k_row < qk || d->k_row >= most)) ||
+        (d->v_row != 0 && (d->v_row < v || d->v_row >= most)) || v >= most)
+        return MFPSN_ERR_SHAPE;
+    if (!isfinite(d->scale))
+        return MFPSN_ERR_PARAM;
+    // blocks of a launch: (sequence, head, chunk), (sequence, head, 32 columns)
+    const int64_t nc = ((int64_t)d->T + kDeltaChunk - 1) / kDeltaChunk, heads = (int64_t)d->N * d->Hv;
+    const int64_t each = nc > 8 ? nc : 8;
+    if (heads > (((int64_t)1 << 31) - 1) / each)
+        return MFPSN_ERR_SHAPE;
+    return MFPSN_OK;
+}
+
+DeltaLayout layout_of(const mfpsn_delta_desc* d)
+{
+    return delta_layout(d->T, d->N, d->Hv, d->Dk, d->Dv, delta_elem(d->dtype));
+}
+
+bool by_steps(const mfpsn_delta_desc* d) { return d->T <= kDeltaStepsMaxT; }
+
+// rows that may be read 16 bytes at a time: the base and every row and head
+// (of `width` elements) start at a multiple of 16 bytes
+bool wide_rows(const void* p, int64_t row, int width, int es)
+{
+    return aligned(p, 16) && row * es % 16 == 0 && width * es % 16 == 0;
+}
+
+void fill(DeltaArgs& a, const mfpsn_delta_desc* d, const void* q, const void* k, const void* v, const void* g,
+          const void* beta, const int32_t* lengths)
+{
+    a = DeltaArgs{};
+    a.T = d->T;
+    a.N = d->N;
+    a.Hk = d->Hk;
+    a.Hv = d->Hv;
+    a.Dk = d->Dk;
+    a.Dv = d->Dv;
+    a.scale = d->scale;
+    a.q_row = d->q_row ? d->q_row : (int64_t)d->Hk * d->Dk;
+    a.k_row = d->k_row ? d->k_row : (int64_t)d->Hk * d->Dk;
+    a.v_row = d->v_row ? d->v_row : (int64_t)d->Hv * d->Dv;
+    const int es = elem_bytes(d->dtype);
+    a.vec_qk = wide_rows(q, a.q_row, d->Dk, es) && wide_rows(k, a.k_row, d->Dk, es);
+    a.nc = (int32_t)(((int64_t)d->T + kDeltaChunk - 1) / kDeltaChunk);
+    a.dvp = (d->Dv + 15) / 16 * 16;
+    a.q = q;
+    a.k = k;
+    a.v = v;
+    a.g = g;
+    a.beta = beta;
+    a.lengths = lengths;
+}
+
+// The arrays of the forward's chunks in `base`
+void place(DeltaArgs& a, const DeltaLayout& l, void* base, bool saved)
+{
+    char* p = (char*)base;
+    a.X = p;
+    p += l.units * l.x;
+    a.P = p;
+    p += l.units * l.p;
+    a.gate = (float*)p;
+    p += l.units * l.gate;
+    if (saved) {
+        a.U = p;
+        p += l.units * l.u;
+        a.S0 = p;
+    }
+}
+
+int check_inputs(const mfpsn_delta_desc* d, const void* q, const void* k, const void* v, const void* g, const void* beta)
+{
+    if (!q || !k || !v || !g || !beta)
+        return MFPSN_ERR_NULL;
+    const int es = elem_bytes(d->dtype);
+    if (!aligned(q, es) || !aligned(k, es) || !aligned(v, es) || !aligned(g, es) || !aligned(beta, es))
+        return MFPSN_ERR_ALIGN;
+    return MFPSN_OK;
+}
+
+}  // namespace
+
+int mfpsn_layer_norm_forward(int64_t M, int32_t C, int32_t S, int32_t dtype, const void* x, const float* gamma,
+                             const float* beta, float eps, void* y, float* mean, float* rstd, void* stream)
+{
+    const int st = validate_norm(M, C, S);
+    if (st != MFPSN_OK)
+        return st;
+    if (!float_dtype(dtype))
+        return MFPSN_ERR_DTYPE;
+    if (!(eps >= 0.0f) || !isfinite(eps))
+        return MFPSN_ERR_PARAM;
+    if ((mean == nullptr) != (rstd == nullptr))
+        return MFPSN_ERR_NULL;
+    const int es = elem_bytes(dtype);
+    if (!aligned(x, es) || !aligned(y, es) || !aligned(gamma, 4) || !aligned(beta, 4) || !aligned(mean, 4) ||
+        !aligned(rstd, 4))
+        return MFPSN_ERR_ALIGN;
+    if (M == 0 || C == 0 || S == 0)
+        return MFPSN_OK;
+    if (!x || !y)
+        return MFPSN_ERR_NULL;
+    NormArgs a{};
+    a.M = M;
+    a.C = C;
+    a.S = S;
+    a.eps = eps;
+    a.x = x;
+    a.gamma = gamma;
+    a.beta = beta;
+    a.mean = mean;
+    a.rstd = rstd;
+    a.out = y;
+    return launch_norm_forward(a, dtype, (hipStream_t)stream) == hipSuccess ? MFPSN_OK : MFPSN_ERR_HIP;
+}
+
+int mfpsn_layer_norm_workspace_size(int64_t M, int32_t C, int32_t S, size_t* bytes)
+{
+    const int st = validate_norm(M, C, S);
+    if (st != MFPSN_OK)
+        return st;
+    if (!bytes)
+        return MFPSN_ERR_NULL;
+    *bytes = (size_t)norm_blocks(M, C, S) * 2 * (size_t)C * sizeof(float);
+    return MFPSN_OK;
+}
+
+int mfpsn_layer_norm_backward(int64_t M, int32_t C, int32_t S, int32_t dtype, const void* x, const float* gamma,
+                              const float* mean, const float* rstd, const void* grad_y, void* grad_x,
+                              float* grad_gamma, float* grad_beta, void* workspace, size_t workspace_bytes,
+                              void* stream)
+{
+    const int st = validate_norm(M, C, S);
+    if (st != MFPSN_OK)
+        return st;
+    if (!float_dtype(dtype))
+        return MFPSN_ERR_DTYPE;
+    const int es = elem_bytes(dtype);
+    if (!aligned(x, es) || !aligned(grad_y, es) || !aligned(grad_x, es) || !aligned(gamma, 4) || !aligned(mean, 4) ||
+        !aligned(rstd, 4) || !aligned(grad_gamma, 4) || !aligned(grad_beta, 4))
+        return MFPSN_ERR_ALIGN;
+    if (C == 0)
+        return MFPSN_OK;
+    const bool empty = M == 0 || S == 0;
+    if (!empty && (!x || !mean || !rstd || !grad_y || !grad_x))
+        return MFPSN_ERR_NULL;
+    const bool weights = grad_gamma || grad_beta;
+    if (weights && (!workspace || !aligned(workspace, 4) ||
+                    workspace_bytes < (size_t)norm_blocks(M, C, S) * 2 * (size_t)C * sizeof(float)))
+        return MFPSN_ERR_WORKSPACE;
+    if (empty && !weights)
+        return MFPSN_OK;
+    NormArgs a{};
+    a.M = empty ? 0 : M;  // (nothing to sum: zero gradients of the weights)
+    a.C = C;
+    a.S = empty ? 1 : S;
+    a.x = x;
+    a.gy = grad_y;
+    a.gamma = gamma;
+    a.mean = const_cast<float*>(mean);
+    a.rstd = const_cast<float*>(rstd);
+    a.out = grad_x;
+    a.part = weights ? (float*)workspace : nullptr;
+    a.grad_gamma = grad_gamma;
+    a.grad_beta = grad_beta;
+    return launch_norm_backward(a, dtype, (hipStream_t)stream) == hipSuccess ? MFPSN_OK : MFPSN_ERR_HIP;
+}
+
+int mfpsn_delta_workspace_size(const mfpsn_delta_desc* desc, size_t* bytes)
+{
+    const int st = validate_delta(desc);
+    if (st != MFPSN_OK)
+        return st;
+    if (!bytes)
+        return MFPSN_ERR_NULL;
+    *bytes = by_steps(desc) ? 0 : layout_of(desc).chunk_bytes();
+    return MFPSN_OK;
+}
+
+int mfpsn_delta_saved_size(const mfpsn_delta_desc* desc, size_t* bytes)
+{
+    const int st = validate_delta(desc);
+    if (st != MFPSN_OK)
+        return st;
+    if (!bytes)
+        return MFPSN_ERR_NULL;
+    *bytes = layout_of(desc).saved_bytes();
+    return MFPSN_OK;
+}
+
+int mfpsn_delta_backward_workspace_size(const mfpsn_delta_desc* desc, size_t* bytes)
+{
+    const int st = validate_delta(desc);
+    if (st != MFPSN_OK)
+        return st;
+    if (!bytes)
+        return MFPSN_ERR_NULL;
+    *bytes = layout_of(desc).grad_bytes();
+    return MFPSN_OK;
+}
+
+int mfpsn_delta_forward(const mfpsn_delta_desc* desc, const void* q, const void* k, const void* v, const void* g,
+                        const void* beta, const int32_t* lengths, const float* state_in, void* o, float* state_out,
+                        void* saved, size_t saved_bytes, void* workspace, size_t workspace_bytes, void* stream)
+{
+    int st = validate_delta(desc);
+    if (st != MFPSN_OK)
+        return st;
+    if (desc->N == 0)
+        return MFPSN_OK;
+    if (desc->T > 0) {
+        st = check_inputs(desc, q, k, v, g, beta);
+        if (st != MFPSN_OK)
+            return st;
+        if (!o)
+            return MFPSN_ERR_NULL;
+    }
+    if (!aligned(o, elem_bytes(desc->dtype)) || !aligned(lengths, 4) || !aligned(state_in, 4) || !aligned(state_out, 4))
+        return MFPSN_ERR_ALIGN;
+    const DeltaLayout l = layout_of(desc);
+    const bool steps = !saved && by_steps(desc);
+    if (saved ? (saved_bytes < l.saved_bytes() || !aligned(saved, 16))
+              : (!steps && (!workspace || workspace_bytes < l.chunk_bytes() || !aligned(workspace, 16))))
+        return MFPSN_ERR_WORKSPACE;
+    DeltaArgs a;
+    fill(a, desc, q, k, v, g, beta, lengths);
+    a.state_in = state_in;
+    a.o = o;
+    a.state_out = state_out;
+    if (!steps)
+        place(a, l, saved ? saved : workspace, saved != nullptr);
+    const hipStream_t s = (hipStream_t)stream;
+    return (steps ? launch_delta_steps(a, desc->dtype, s) : launch_delta_forward(a, desc->dtype, s)) == hipSuccess
+               ? MFPSN_OK
+               : MFPSN_ERR_HIP;
+}
+
+int mfpsn_delta_backward(const mfpsn_delta_desc* desc, const void* q, const void* k, const void* v, const void* g,
+                         const void* beta, const int32_t* lengths, const void* saved, size_t saved_bytes,
+                         const void* grad_o, const float* grad_state_out, void* grad_q, void* grad_k, void* grad_v,
+                         void* grad_g, void* grad_beta, float* grad_state_in, void* workspace,
+                         size_t workspace_bytes, void* stream)
+{
+    int st = validate_delta(desc);
+    if (st != MFPSN_OK)
+        return st;
+    if (desc->N == 0)
+        return MFPSN_OK;
+    const int es = elem_bytes(desc->dtype);
+    if (desc->T > 0) {
+        st = check_inputs(desc, q, k, v, g, beta);
+        if (st != MFPSN_OK)
+            return st;
+        if (!grad_o || !grad_q || !grad_k || !grad_v || !grad_g || !grad_beta)
+            return MFPSN_ERR_NULL;
+    }
+    if (!aligned(grad_o, es) || !aligned(grad_q, es) || !aligned(grad_k, es) || !aligned(grad_v, es) ||
+        !aligned(grad_g, es) || !aligned(grad_beta, es) || !aligned(lengths, 4) || !aligned(grad_state_out, 4) ||
+        !aligned(grad_state_in, 4))
+        return MFPSN_ERR_ALIGN;
+    const DeltaLayout l = layout_of(desc);
+    if (desc->T > 0 && (!saved || saved_bytes < l.saved_bytes() || !aligned(saved, 16) || !workspace ||
+                        workspace_bytes < l.grad_bytes() || !aligned(workspace, 16)))
+        return MFPSN_ERR_WORKSPACE;
+    DeltaArgs a;
+    fill(a, desc, q, k, v, g, beta, lengths);
+    place(a, l, const_cast<void*>(saved), true);
+    a.vec_v = wide_rows(grad_o, (int64_t)desc->Hv * desc->Dv, desc->Dv, es) &&
+              wide_rows(grad_v, (int64_t)desc->Hv * desc->Dv, desc->Dv, es);
+    a.grad_o = grad_o;
+    a.grad_state_out = grad_state_out;
+    a.dS = workspace;
+    a.grad_q = grad_q;
+    a.grad_k = grad_k;
+    a.grad_v = grad_v;
+    a.grad_g = grad_g;
+    a.grad_beta = grad_beta;
+    a.grad_state_in = grad_state_in;
+    return launch_delta_backward(a, desc->dtype, (hipStream_t)stream) == hipSuccess ? MFPSN_OK : MFPSN_ERR_HIP;
+}
+
+int mfpsn_delta_step(const mfpsn_delta_desc* desc, const void* q, const void* k, const void* v, const void* g,
+                     const void* beta, const float* state_in, void* o, float* state_out, void* stream)
+{
+    if (!desc)
+        return MFPSN_ERR_NULL;
+    mfpsn_delta_desc one = *desc;
+    one.T = 1;
+    int st = validate_delta(&one);
+    if (st != MFPSN_OK)
+        return st;
+    if (one.N == 0)
+        return MFPSN_OK;
+    st = check_inputs(&one, q, k, v, g, beta);
+    if (st != MFPSN_OK)
+        return st;
+    if (!o || !state_out)
+        return MFPSN_ERR_NULL;
+    if (!aligned(o, elem_bytes(one.dtype)) || !aligned(state_in, 4) || !aligned(state_out, 4))
+        return MFPSN_ERR_ALIGN;
+    DeltaArgs a;
+    fill(a, &one, q, k, v, g, beta, nullptr);
+    a.state_in = state_in;
+    a.o = o;
+    a.state_out = state_out;
+    return launch_delta_steps(a, one.dtype, (hipStream_t)stream) == hipSuccess ? MFPSN_OK : MFPSN_ERR_HIP;
+}

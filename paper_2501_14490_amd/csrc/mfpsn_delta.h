@@ -1,0 +1,76 @@
+// Internal interface of the gated-delta-rule kernels (mfpsn_delta.hip,
+// mfpsn_delta_step.hip) for the C-ABI layer.  Not installed; not part of the
+// ABI.
+#pragma once
+
+#include <hip/hip_runtime_api.h>
+#include <stddef.h>
+#include <stdint.h>
+
+namespace mfpsn {
+
+constexpr int kDeltaChunk = 64;   // time steps of one chunk
+constexpr int kDeltaMaxDk = 128;  // longest key
+constexpr int kDeltaMaxDv = 256;  // longest value
+// Longest sequences that launch_delta_steps takes in the forward (nothing saved)
+constexpr int kDeltaStepsMaxT = 8;
+
+struct DeltaArgs {
+    int32_t T, N, Hk, Hv, Dk, Dv;
+    float scale;
+    int64_t q_row, k_row, v_row;  // elements between the rows of consecutive (t, n)
+    int32_t vec_qk, vec_v;        // rows of q and k (of v) may be read 16 bytes at a time
+    int32_t nc;                   // chunks of the longest sequence
+    int32_t dvp;                  // Dv rounded up to 16
+    const void *q, *k, *v, *g, *beta;
+    const int32_t* lengths;       // nullable: T for every sequence
+    const float* state_in;        // nullable: zeros
+    void* o;
+    float* state_out;             // nullable
+    // per (sequence, value head, chunk), see delta_layout
+    void *X, *P, *S0, *U;         // S0, U: nullable in the forward (not saved)
+    float* gate;                  // [2][64]: e^G, e^(G_last - G)
+    // backward
+    const void* grad_o;
+    const float* grad_state_out;  // nullable: zeros
+    void* dS;                     // gradient of the state behind each chunk
+    void *grad_q, *grad_k, *grad_v, *grad_g, *grad_beta;
+    float* grad_state_in;         // nullable
+};
+
+// Bytes a (sequence, value head, chunk) takes of each array: X (16-bit: a high
+// and a low part), P, the gates; U and S0 (what the backward needs besides).
+struct DeltaLayout {
+    size_t units;                     // sequences x value heads x chunks
+    size_t x, p, gate, u, s0;         // bytes of each unit
+    size_t chunk_bytes() const { return units * (x + p + gate); }
+    size_t saved_bytes() const { return units * (x + p + gate + u + s0); }
+    size_t grad_bytes() const { return units * s0; }
+};
+
+// Bytes of an element of P, U, S0 and dS: what the matrix products take
+constexpr bool kDeltaBf16Products = false;
+inline int delta_elem(int dtype) { return kDeltaBf16Products && dtype == 1 ? 2 : 4; }
+
+inline int delta_dkp(int Dk) { return Dk <= 64 ? 64 : 128; }
+
+// es: delta_elem
+inline DeltaLayout delta_layout(int64_t T, int64_t N, int64_t Hv, int Dk, int Dv, int es)
+{
+    DeltaLayout l;
+    const size_t L = kDeltaChunk, dvp = (size_t)(Dv + 15) / 16 * 16, dkp = (size_t)delta_dkp(Dk);
+    l.units = (size_t)N * (size_t)Hv * (size_t)((T + kDeltaChunk - 1) / kDeltaChunk);
+    l.x = L * L * 4;
+    l.p = L * L * (size_t)es;
+    l.gate = 2 * L * 4;
+    l.u = dvp * L * (size_t)es;
+    l.s0 = dvp * dkp * (size_t)es;
+    return l;
+}
+
+hipError_t launch_delta_forward(const DeltaArgs& a, int dtype, hipStream_t stream);
+hipError_t launch_delta_backward(const DeltaArgs& a, int dtype, hipStream_t stream);
+// One step after another in one kernel, the state in registers
+hipError_t launch_delta_steps(const DeltaArgs& a, int dtype, hipStream_t stream);
+
+}  // namespace mfpsn

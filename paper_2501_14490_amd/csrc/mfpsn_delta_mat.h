@@ -1,0 +1,172 @@
+// 16x16 matrix products of one wave on gfx950's matrix cores, as the
+// gated-delta-rule kernels use them: operands from LDS, or a result fed back
+// as the next product's right operand without leaving the registers.
+//
+// A result tile D (16x16) has column lane % 16 in a lane, rows 4 g + r in its
+// register r, g = lane / 16.  A right operand needs column lane % 16 too, and
+// for its contraction index any fixed order, as long as the left operand has
+// the same.  So the order is chosen such that a result's registers are a
+// right operand as they are: f32 contracts one tile's 16 rows in four
+// v_mfma_f32_16x16x4_f32, number r over the rows {4 g + r}; bf16 contracts two
+// tiles' 32 rows in one v_mfma_f32_16x16x32_bf16, lane group g over the rows
+// 4 g .. 4 g + 3 of the first tile, then those of the second.  A chain of
+// products (state -> residuals -> values -> state) then needs no LDS round
+// trip and no barrier.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace mfpsn {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef short i16x4 __attribute__((ext_vector_type(4)));
+
+__device__ __forceinline__ f32x4 mfma_f32(const f32x4 a, const f32x4 b, f32x4 c)
+{
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+        c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[r], b[r], c, 0, 0, 0);
+    return c;
+}
+
+template <bool BF> struct Mat;
+
+template <> struct Mat<false> {
+    using El = float;
+    using Frag = f32x4;
+    static constexpr int KU = 16;   // rows that one product contracts
+    static constexpr int TU = 1;    // result tiles that make one right operand
+    static constexpr int PAD = 4;   // elements between the rows of an LDS tile: rows start 4 banks apart
+    // operand from LDS [m][k]: rows m0 .. m0 + 15 (p points at row m0), contraction block u
+    __device__ static Frag rows(const El* p, int ld, int u)
+    {
+        const int lane = threadIdx.x & 63;
+        return *(const f32x4*)(p + (lane & 15) * ld + 16 * u + 4 * (lane >> 4));
+    }
+    // operand from LDS [k][m]: columns 0 .. 15 of p
+    __device__ static Frag cols(const El* p, int ld, int u)
+    {
+        const int lane = threadIdx.x & 63;
+        const El* s = p + (16 * u + 4 * (lane >> 4)) * ld + (lane & 15);
+        return f32x4{s[0], s[ld], s[2 * ld], s[3 * ld]};
+    }
+    __device__ static Frag pack(const f32x4* t) { return t[0]; }
+    __device__ static f32x4 mma(Frag a, Frag b, f32x4 c) { return mfma_f32(a, b, c); }
+    __device__ static El put(float v) { return v; }
+    __device__ static float get(El v) { return v; }
+};
+
+template <> struct Mat<true> {
+    using El = __bf16;
+    using Frag = bf16x8;
+    static constexpr int KU = 32, TU = 2, PAD = 8;
+    __device__ static Frag join(bf16x4 a, bf16x4 b) { return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7); }
+    __device__ static Frag rows(const El* p, int ld, int u)
+    {
+        const int lane = threadIdx.x & 63;
+        const El* s = p + (lane & 15) * ld + 32 * u + 4 * (lane >> 4);
+        return join(*(const bf16x4*)s, *(const bf16x4*)(s + 16));
+    }
+    // 16 lanes read 4 rows of 16 columns, 8 bytes each, and get a column's 4 rows each
+    __device__ static bf16x4 transposed(const El* p)
+    {
+        const i16x4 v = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4*)p);
+        return __builtin_bit_cast(bf16x4, v);
+    }
+    __device__ static Frag cols(const El* p, int ld, int u)
+    {
+        const int lane = threadIdx.x & 63, i = lane & 15;
+        const El* s = p + (32 * u + 4 * (lane >> 4) + (i >> 2)) * ld + 4 * (i & 3);
+        return join(transposed(s), transposed(s + 16 * ld));
+    }
+    __device__ static Frag pack(const f32x4* t)
+    {
+        Frag f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            f[i] = (__bf16)t[i >> 2][i & 3];
+        return f;
+    }
+    // what pack() left of each value, as the next 8 bits
+    __device__ static Frag pack_rest(const f32x4* t, Frag hi)
+    {
+        Frag f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            f[i] = (__bf16)(t[i >> 2][i & 3] - (float)hi[i]);
+        return f;
+    }
+    __device__ static f32x4 mma(Frag a, Frag b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+    __device__ static El put(float v) { return (__bf16)v; }
+    __device__ static float get(El v) { return (float)v; }
+};
+
+// Storage types of the tensors
+struct StoreF32 {
+    using T = float;
+    __device__ static float get(T v) { return v; }
+    __device__ static T put(float v) { return v; }
+};
+struct StoreBF16 {
+    using T = __bf16;
+    __device__ static float get(T v) { return (float)v; }
+    __device__ static T put(float v) { return (__bf16)v; }  // to nearest even
+};
+
+// 64 rows of `cols` elements from memory (`stride` elements apart; rows from
+// `live` on are not read) into LDS rows of `ld` elements, zeros behind `live` and
+// from `cols` up to COLS.  vec: rows are 16-byte aligned and cols a multiple of 16 bytes.
+template <typename D, typename El, int COLS, int THREADS, int ROWS = 64>
+__device__ __forceinline__ void stage(El* lds, int ld, const typename D::T* src, int64_t stride, int live, int cols,
+                                      bool vec)
+{
+    using T = typename D::T;
+    constexpr int VE = 16 / sizeof(T), PER = COLS / VE;
+    static_assert(COLS % VE == 0);
+    for (int i = threadIdx.x; i < ROWS * PER; i += THREADS) {
+        const int r = i / PER, c = (i - r * PER) * VE;
+        alignas(16) T e[VE];
+#pragma unroll
+        for (int j = 0; j < VE; ++j)
+            e[j] = D::put(0.0f);
+        if (r < live && c < cols) {
+            const T* s = src + (int64_t)r * stride + c;
+            if (vec) {
+                *(uint4*)e = *(const uint4*)s;
+            } else {
+#pragma unroll
+                for (int j = 0; j < VE; ++j)
+                    if (c + j < cols)
+                        e[j] = s[j];
+            }
+        }
+        El* d = lds + r * ld + c;
+        if constexpr (sizeof(El) == sizeof(T)) {
+            *(uint4*)d = *(const uint4*)e;
+        } else {
+#pragma unroll
+            for (int j = 0; j < VE; ++j)
+                d[j] = (El)D::get(e[j]);
+        }
+    }
+}
+
+// ROWS x COLS elements lying densely in memory into LDS rows of `ld` elements;
+// rows from `live` on become zeros
+template <typename El, int ROWS, int COLS, int THREADS>
+__device__ __forceinline__ void stage_dense(El* lds, int ld, const El* src, int live = ROWS)
+{
+    constexpr int VE = 16 / sizeof(El), PER = COLS / VE;
+    for (int i = threadIdx.x; i < ROWS * PER; i += THREADS) {
+        const int r = i / PER, c = (i - r * PER) * VE;
+        uint4 v = {0, 0, 0, 0};
+        if (r < live)
+            v = *(const uint4*)(src + (int64_t)r * COLS + c);
+        *(uint4*)(lds + r * ld + c) = v;
+    }
+}
+
+}  // namespace mfpsn

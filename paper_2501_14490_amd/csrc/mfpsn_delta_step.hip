@@ -1,0 +1,198 @@
+// gfx950 kernel of the gated delta rule, one time step after another:
+//   S_t = e^g S_{t-1} + beta k (v - e^g S_{t-1}^T k)^T,   o = scale S_t^T q
+// for a single arriving step (serving) and for sequences too short for the
+// chunked form to pay.  The state (float [N][Hv][Dk][Dv]) is read once, kept in
+// registers over the steps and written once: a single step is bound by those
+// two passes over HBM.
+//
+// A block of 256 threads has 32 columns of one head's state: 8 lanes of 4
+// neighbouring columns (128 bytes of a row) by 32 groups of rows, Dk/32 rows a
+// thread, so a head of 128 columns is spread over 4 blocks (a lone stream of a
+// few heads would otherwise leave most of the chip idle).  S_t^T q is taken as
+//   e^g S_{t-1}^T q + (k.q) u,   u = beta (v - e^g S_{t-1}^T k),
+// so both products of a step read the old state and their partial sums meet in
+// one reduction (lanes, then the four waves through LDS, one barrier a step).
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "mfpsn_delta.h"
+#include "mfpsn_internal.h"
+
+namespace mfpsn {
+namespace {
+
+struct F32 {
+    using T = float;
+    __device__ static float get(T v) { return v; }
+    __device__ static T put(float v) { return v; }
+};
+struct BF16 {
+    using T = uint16_t;
+    __device__ static float get(T v) { return __builtin_bit_cast(float, (uint32_t)v << 16); }
+    __device__ static T put(float v) { return __builtin_bit_cast(uint16_t, (__bf16)v); }
+};
+
+constexpr int kCols = 32, kGroups = 32;
+
+// R: rows of the state a thread has, ceil(Dk / 32); VEC: the rows of the state
+// are 16-byte aligned
+template <typename D, int R, bool VEC>
+__global__ __launch_bounds__(256) void delta_steps_kernel(DeltaArgs a)
+{
+    using T = typename D::T;
+    __shared__ float part[2][4][9][8];
+    const int tid = threadIdx.x, lc = tid & 7, rg = tid >> 3, wave = tid >> 6, lane = tid & 63;
+    const int vblocks = (a.Dv + kCols - 1) / kCols;
+    const int64_t head = blockIdx.x / vblocks;  // n * Hv + hv
+    const int n = (int)(head / a.Hv), hv = (int)(head - (int64_t)n * a.Hv), hk = hv / (a.Hv / a.Hk);
+    const int v0 = (int)(blockIdx.x % vblocks) * kCols + lc * 4;
+    const int len = a.lengths ? min(max(a.lengths[n], 0), a.T) : a.T;
+
+    float S[R][4];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        const int d = rg + kGroups * r;
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+            S[r][c] = 0.0f;
+        if (a.state_in && d < a.Dk) {
+            const float* p = a.state_in + (head * a.Dk + d) * a.Dv + v0;
+            if (VEC) {
+                if (v0 < a.Dv) {
+                    const float4 f = *(const float4*)p;
+                    S[r][0] = f.x;
+                    S[r][1] = f.y;
+                    S[r][2] = f.z;
+                    S[r][3] = f.w;
+                }
+            } else {
+#pragma unroll
+                for (int c = 0; c < 4; ++c)
+                    if (v0 + c < a.Dv)
+                        S[r][c] = p[c];
+            }
+        }
+    }
+    float q[R], k[R], v[4], g, beta;
+    const auto fetch = [&](int t) {
+        const int64_t row = (int64_t)t * a.N + n;
+        const T* __restrict__ pq = (const T*)a.q + row * a.q_row + (int64_t)hk * a.Dk;
+        const T* __restrict__ pk = (const T*)a.k + row * a.k_row + (int64_t)hk * a.Dk;
+        const T* __restrict__ pv = (const T*)a.v + row * a.v_row + (int64_t)hv * a.Dv;
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            const int d = rg + kGroups * r;
+            q[r] = d < a.Dk ? D::get(pq[d]) : 0.0f;
+            k[r] = d < a.Dk ? D::get(pk[d]) : 0.0f;
+        }
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+            v[c] = v0 + c < a.Dv ? D::get(pv[v0 + c]) : 0.0f;
+        g = D::get(((const T*)a.g)[row * a.Hv + hv]);
+        beta = D::get(((const T*)a.beta)[row * a.Hv + hv]);
+    };
+    if (len > 0)
+        fetch(0);
+    for (int t = 0; t < len; ++t) {
+        float sum[9] = {};  // S^T k, S^T q, k.q
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                sum[c] = __builtin_fmaf(S[r][c], k[r], sum[c]);
+                sum[4 + c] = __builtin_fmaf(S[r][c], q[r], sum[4 + c]);
+            }
+            sum[8] = __builtin_fmaf(k[r], q[r], sum[8]);
+        }
+#pragma unroll
+        for (int o = 8; o < 64; o <<= 1)
+#pragma unroll
+            for (int i = 0; i < 9; ++i)
+                sum[i] += __shfl_xor(sum[i], o);
+        float(*buf)[9][8] = part[t & 1];
+        if (lane < 8)
+#pragma unroll
+            for (int i = 0; i < 9; ++i)
+                buf[wave][i][lane] = sum[i];
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < 9; ++i)
+            sum[i] = (buf[0][i][lc] + buf[1][i][lc]) + (buf[2][i][lc] + buf[3][i][lc]);
+        const float decay = expf(g);
+        float u[4], o[4];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            u[c] = beta * (v[c] - decay * sum[c]);
+            o[c] = a.scale * __builtin_fmaf(sum[8], u[c], decay * sum[4 + c]);
+        }
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+            for (int c = 0; c < 4; ++c)
+                S[r][c] = __builtin_fmaf(k[r], u[c], decay * S[r][c]);
+        if (t + 1 < len)
+            fetch(t + 1);
+        if (rg == 0) {
+            T* __restrict__ po = (T*)a.o + (((int64_t)t * a.N + n) * a.Hv + hv) * a.Dv;
+#pragma unroll
+            for (int c = 0; c < 4; ++c)
+                if (v0 + c < a.Dv)
+                    po[v0 + c] = D::put(o[c]);
+        }
+    }
+    for (int t = len + rg; t < a.T; t += kGroups) {  // steps behind the sequence's end
+        T* __restrict__ po = (T*)a.o + (((int64_t)t * a.N + n) * a.Hv + hv) * a.Dv;
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+            if (v0 + c < a.Dv)
+                po[v0 + c] = D::put(0.0f);
+    }
+    if (!a.state_out)
+        return;
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        const int d = rg + kGroups * r;
+        if (d < a.Dk) {
+            float* p = a.state_out + (head * a.Dk + d) * a.Dv + v0;
+            if (VEC) {
+                if (v0 < a.Dv)
+                    *(float4*)p = make_float4(S[r][0], S[r][1], S[r][2], S[r][3]);
+            } else {
+#pragma unroll
+                for (int c = 0; c < 4; ++c)
+                    if (v0 + c < a.Dv)
+                        p[c] = S[r][c];
+            }
+        }
+    }
+}
+
+template <typename D, int R> hipError_t go(const DeltaArgs& a, hipStream_t s)
+{
+    const bool vec = a.Dv % 4 == 0 && (uintptr_t)a.state_in % 16 == 0 && (uintptr_t)a.state_out % 16 == 0;
+    const dim3 grid((unsigned)((int64_t)a.N * a.Hv * ((a.Dv + kCols - 1) / kCols)));
+    if (vec)
+        delta_steps_kernel<D, R, true><<<grid, dim3(256), 0, s>>>(a);
+    else
+        delta_steps_kernel<D, R, false><<<grid, dim3(256), 0, s>>>(a);
+    return hipGetLastError();
+}
+
+template <typename D> hipError_t by_rows(const DeltaArgs& a, hipStream_t s)
+{
+    switch ((a.Dk + kGroups - 1) / kGroups) {
+    case 1: return go<D, 1>(a, s);
+    case 2: return go<D, 2>(a, s);
+    case 3: return go<D, 3>(a, s);
+    default: return go<D, 4>(a, s);
+    }
+}
+
+}  // namespace
+
+hipError_t launch_delta_steps(const DeltaArgs& a, int dtype, hipStream_t stream)
+{
+    return dtype == kBF16 ? by_rows<BF16>(a, stream) : by_rows<F32>(a, stream);
+}
+
+}  // namespace mfpsn

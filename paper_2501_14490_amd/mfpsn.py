@@ -51,6 +51,12 @@ class MfpsnDesc(ctypes.Structure):
                 ("shift_hi", ctypes.c_int32)]
 
 
+class MfpsnDeltaDesc(ctypes.Structure):
+    _fields_ = [("T", ctypes.c_int32), ("N", ctypes.c_int32), ("Hk", ctypes.c_int32), ("Hv", ctypes.c_int32),
+                ("Dk", ctypes.c_int32), ("Dv", ctypes.c_int32), ("dtype", ctypes.c_int32), ("scale", ctypes.c_float),
+                ("q_row", ctypes.c_int64), ("k_row", ctypes.c_int64), ("v_row", ctypes.c_int64)]
+
+
 _P = ctypes.c_void_p
 _DP = ctypes.POINTER(MfpsnDesc)
 _lib.mfpsn_forward.argtypes = [_DP, _P, _P, _P, _P, _P, _P, _P, _P, _P]
@@ -90,6 +96,20 @@ _lib.mfpsn_sawtooth_dilation.argtypes = [ctypes.c_int32, ctypes.c_int32]
 _lib.mfpsn_sawtooth_dilation.restype = ctypes.c_int32
 _lib.mfpsn_status_string.argtypes = [ctypes.c_int]
 _lib.mfpsn_status_string.restype = ctypes.c_char_p
+_I32, _I64, _SZ, _SZP = ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t, ctypes.POINTER(ctypes.c_size_t)
+_DDP = ctypes.POINTER(MfpsnDeltaDesc)
+_lib.mfpsn_layer_norm_forward.argtypes = [_I64, _I32, _I32, _I32, _P, _P, _P, ctypes.c_float, _P, _P, _P, _P]
+_lib.mfpsn_layer_norm_workspace_size.argtypes = [_I64, _I32, _I32, _SZP]
+_lib.mfpsn_layer_norm_backward.argtypes = [_I64, _I32, _I32, _I32] + [_P] * 9 + [_SZ, _P]
+_lib.mfpsn_delta_workspace_size.argtypes = [_DDP, _SZP]
+_lib.mfpsn_delta_saved_size.argtypes = [_DDP, _SZP]
+_lib.mfpsn_delta_backward_workspace_size.argtypes = [_DDP, _SZP]
+_lib.mfpsn_delta_forward.argtypes = [_DDP] + [_P] * 10 + [_SZ, _P, _SZ, _P]
+_lib.mfpsn_delta_backward.argtypes = [_DDP] + [_P] * 7 + [_SZ] + [_P] * 9 + [_SZ, _P]
+_lib.mfpsn_delta_step.argtypes = [_DDP] + [_P] * 9
+for _name in ("layer_norm_forward", "layer_norm_workspace_size", "layer_norm_backward", "delta_workspace_size",
+              "delta_saved_size", "delta_backward_workspace_size", "delta_forward", "delta_backward", "delta_step"):
+    getattr(_lib, "mfpsn_" + _name).restype = ctypes.c_int
 _lib.mfpsn_abi_version.argtypes = []
 _lib.mfpsn_abi_version.restype = ctypes.c_int32
 
@@ -258,6 +278,68 @@ def mfpsn_stream_step(desc: MfpsnDesc, t: int, x_t, ring, sign, shift, bias, spi
                       stream=None) -> None:
     _check(_lib.mfpsn_stream_step(ctypes.byref(desc), int(t), _ptr(x_t), _ptr(ring), _ptr(sign), _ptr(shift),
                                   _ptr(bias), _ptr(spikes_t), _ptr(h_t), _stream(stream)), "mfpsn_stream_step")
+
+
+def _nbytes(t) -> int:
+    return t.numel() * t.element_size() if t is not None else 0
+
+
+def _size(fn, *args) -> int:
+    n = ctypes.c_size_t(0)
+    _check(fn(*args, ctypes.byref(n)), fn.__name__)
+    return int(n.value)
+
+
+def mfpsn_layer_norm_forward(M: int, C: int, S: int, dtype: int, x, gamma, beta, eps: float, y, mean=None, rstd=None,
+                             stream=None) -> None:
+    _check(_lib.mfpsn_layer_norm_forward(int(M), int(C), int(S), int(dtype), _ptr(x), _ptr(gamma), _ptr(beta),
+                                         float(eps), _ptr(y), _ptr(mean), _ptr(rstd), _stream(stream)),
+           "mfpsn_layer_norm_forward")
+
+
+def mfpsn_layer_norm_workspace_size(M: int, C: int, S: int) -> int:
+    return _size(_lib.mfpsn_layer_norm_workspace_size, int(M), int(C), int(S))
+
+
+def mfpsn_layer_norm_backward(M: int, C: int, S: int, dtype: int, x, gamma, mean, rstd, grad_y, grad_x, grad_gamma,
+                              grad_beta, workspace, stream=None) -> None:
+    _check(_lib.mfpsn_layer_norm_backward(int(M), int(C), int(S), int(dtype), _ptr(x), _ptr(gamma), _ptr(mean),
+                                          _ptr(rstd), _ptr(grad_y), _ptr(grad_x), _ptr(grad_gamma), _ptr(grad_beta),
+                                          _ptr(workspace), _nbytes(workspace), _stream(stream)),
+           "mfpsn_layer_norm_backward")
+
+
+def mfpsn_delta_workspace_size(desc: MfpsnDeltaDesc) -> int:
+    return _size(_lib.mfpsn_delta_workspace_size, ctypes.byref(desc))
+
+
+def mfpsn_delta_saved_size(desc: MfpsnDeltaDesc) -> int:
+    return _size(_lib.mfpsn_delta_saved_size, ctypes.byref(desc))
+
+
+def mfpsn_delta_backward_workspace_size(desc: MfpsnDeltaDesc) -> int:
+    return _size(_lib.mfpsn_delta_backward_workspace_size, ctypes.byref(desc))
+
+
+def mfpsn_delta_forward(desc: MfpsnDeltaDesc, q, k, v, g, beta, lengths, state_in, o, state_out, saved, workspace,
+                        stream=None) -> None:
+    _check(_lib.mfpsn_delta_forward(ctypes.byref(desc), _ptr(q), _ptr(k), _ptr(v), _ptr(g), _ptr(beta), _ptr(lengths),
+                                    _ptr(state_in), _ptr(o), _ptr(state_out), _ptr(saved), _nbytes(saved),
+                                    _ptr(workspace), _nbytes(workspace), _stream(stream)), "mfpsn_delta_forward")
+
+
+def mfpsn_delta_backward(desc: MfpsnDeltaDesc, q, k, v, g, beta, lengths, saved, grad_o, grad_state_out, grad_q,
+                         grad_k, grad_v, grad_g, grad_beta, grad_state_in, workspace, stream=None) -> None:
+    _check(_lib.mfpsn_delta_backward(ctypes.byref(desc), _ptr(q), _ptr(k), _ptr(v), _ptr(g), _ptr(beta),
+                                     _ptr(lengths), _ptr(saved), _nbytes(saved), _ptr(grad_o), _ptr(grad_state_out),
+                                     _ptr(grad_q), _ptr(grad_k), _ptr(grad_v), _ptr(grad_g), _ptr(grad_beta),
+                                     _ptr(grad_state_in), _ptr(workspace), _nbytes(workspace), _stream(stream)),
+           "mfpsn_delta_backward")
+
+
+def mfpsn_delta_step(desc: MfpsnDeltaDesc, q, k, v, g, beta, state_in, o, state_out, stream=None) -> None:
+    _check(_lib.mfpsn_delta_step(ctypes.byref(desc), _ptr(q), _ptr(k), _ptr(v), _ptr(g), _ptr(beta), _ptr(state_in),
+                                 _ptr(o), _ptr(state_out), _stream(stream)), "mfpsn_delta_step")
 
 
 # ---------------------------------------------------------------------------
@@ -530,3 +612,297 @@ class MfPSNBNFunction(torch.autograd.Function):
         grad_w, grad_gamma, grad_beta = bn_backward(ctx.desc, xc, wc, aux, grad_wf, grad_bf, grad_x, ctx.eps,
                                                     ctx.ws)
         return grad_x, grad_w, grad_gamma, grad_beta, None, None, None, None, None, None, None
+
+
+# ---------------------------------------------------------------------------
+# layer norm over the channels
+# ---------------------------------------------------------------------------
+FLOAT_DTYPES = {torch.float32: MFPSN_F32, torch.bfloat16: MFPSN_BF16}
+
+
+def _float_dtype(t, name):
+    if t.dtype not in FLOAT_DTYPES:
+        raise TypeError(f"{name} must be torch.float32 or torch.bfloat16, got {t.dtype}")
+    return FLOAT_DTYPES[t.dtype]
+
+
+def _shaped(t, dtype, device, shape, name):
+    _expect(t, dtype, device, name)
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
+
+
+def _on(device, stream):
+    """The device a call's tensors are on, as the current one, and the stream it goes to."""
+    if device.type != "cuda":
+        raise ValueError(f"tensors must be on a GPU, got {device}")
+    return torch.cuda.device(device), stream if stream is not None else torch.cuda.current_stream(device)
+
+
+def _norm_sizes(x, axis):
+    if not -x.dim() <= axis < x.dim():
+        raise ValueError(f"axis {axis} is none of x's {x.dim()}")
+    axis %= x.dim()
+    M, S = 1, 1
+    for n in x.shape[:axis]:
+        M *= int(n)
+    for n in x.shape[axis + 1:]:
+        S *= int(n)
+    return M, int(x.shape[axis]), S
+
+
+def layer_norm_forward(x, gamma=None, beta=None, eps: float = 1e-5, axis: int = 2, want_stats: bool = False,
+                       stream=None):
+    """y, plus the statistics mean and rstd (float, x's shape without `axis`)
+    with want_stats.  axis: the channels, 2 for time-first tensors
+    [T, N, C, *spatial], 1 for time-last ones [N, C, *spatial, T].
+    gamma, beta: float [C] or None."""
+    dev = x.device
+    dt = _float_dtype(x, "x")
+    _expect(x, x.dtype, dev, "x")
+    M, C, S = _norm_sizes(x, axis)
+    for t, name in ((gamma, "gamma"), (beta, "beta")):
+        if t is not None:
+            _shaped(t, torch.float32, dev, (C,), name)
+    guard, stream = _on(dev, stream)
+    with guard:
+        y = torch.empty_like(x)
+        mean = rstd = None
+        if want_stats:
+            shape = list(x.shape)
+            del shape[axis % x.dim()]
+            mean, rstd = (torch.empty(shape, dtype=torch.float32, device=dev) for _ in range(2))
+        mfpsn_layer_norm_forward(M, C, S, dt, x, gamma, beta, eps, y, mean, rstd, stream)
+    return (y, mean, rstd) if want_stats else y
+
+
+def layer_norm_backward(x, gamma, mean, rstd, grad_y, axis: int = 2, want_weights: bool = True, workspace=None,
+                        stream=None):
+    """grad_x, grad_gamma, grad_beta (grad_x alone without want_weights) from
+    the statistics of layer_norm_forward."""
+    dev = x.device
+    dt = _float_dtype(x, "x")
+    _expect(x, x.dtype, dev, "x")
+    M, C, S = _norm_sizes(x, axis)
+    _shaped(grad_y, x.dtype, dev, x.shape, "grad_y")
+    if gamma is not None:
+        _shaped(gamma, torch.float32, dev, (C,), "gamma")
+    for t, name in ((mean, "mean"), (rstd, "rstd")):
+        _expect(t, torch.float32, dev, name)
+        if t.numel() != M * S:
+            raise ValueError(f"{name} must have {M * S} values, got {t.numel()}")
+    guard, stream = _on(dev, stream)
+    with guard:
+        grad_x = torch.empty_like(x)
+        if not want_weights:
+            mfpsn_layer_norm_backward(M, C, S, dt, x, gamma, mean, rstd, grad_y, grad_x, None, None, None, stream)
+            return grad_x
+        grad_gamma, grad_beta = (torch.empty((C,), dtype=torch.float32, device=dev) for _ in range(2))
+        need = mfpsn_layer_norm_workspace_size(M, C, S)
+        if workspace is None or _nbytes(workspace) < need:
+            workspace = torch.empty(max(need, 8), dtype=torch.uint8, device=dev)
+        mfpsn_layer_norm_backward(M, C, S, dt, x, gamma, mean, rstd, grad_y, grad_x, grad_gamma, grad_beta, workspace,
+                                  stream)
+    return grad_x, grad_gamma, grad_beta
+
+
+class LayerNormFunction(torch.autograd.Function):
+    """y = gamma (x - mean)/sqrt(var + eps) + beta over the channels (axis) of
+    a float32 or bfloat16 x; gamma and beta: [C] or None."""
+
+    @staticmethod
+    def forward(ctx, x, gamma, beta, eps=1e-5, axis=2):
+        xc = x.detach().contiguous()
+        gc, bc = (t.detach().float().contiguous() if t is not None else None for t in (gamma, beta))
+        y, mean, rstd = layer_norm_forward(xc, gc, bc, eps, axis, want_stats=True)
+        ctx.save_for_backward(xc, gc, mean, rstd)
+        ctx.axis = axis
+        ctx.dtypes = [t.dtype if t is not None else None for t in (gamma, beta)]
+        return y
+
+    @staticmethod
+    def backward(ctx, grad_y):
+        xc, gc, mean, rstd = ctx.saved_tensors
+        gy = grad_y.to(xc.dtype).contiguous()
+        want = [ctx.needs_input_grad[1], ctx.needs_input_grad[2]]
+        if not any(want):
+            return layer_norm_backward(xc, gc, mean, rstd, gy, ctx.axis, want_weights=False), None, None, None, None
+        grad_x, gg, gb = layer_norm_backward(xc, gc, mean, rstd, gy, ctx.axis)
+        return (grad_x, gg.to(ctx.dtypes[0]) if want[0] else None, gb.to(ctx.dtypes[1]) if want[1] else None, None,
+                None)
+
+
+# ---------------------------------------------------------------------------
+# gated delta rule
+# ---------------------------------------------------------------------------
+def make_delta_desc(qk_shape, v_shape, dtype="f32", scale=None) -> MfpsnDeltaDesc:
+    """Descriptor for q, k [T, N, Hk, Dk] and v [T, N, Hv, Dv] (time-first);
+    scale: of the outputs, 1/sqrt(Dk) if None."""
+    T, N, Hk, Dk = (int(n) for n in qk_shape)
+    Tv, Nv, Hv, Dv = (int(n) for n in v_shape)
+    if (T, N) != (Tv, Nv):
+        raise ValueError(f"q and k {tuple(qk_shape)} and v {tuple(v_shape)} differ in steps or sequences")
+    dt = DTYPES[dtype] if isinstance(dtype, str) else int(dtype)
+    return MfpsnDeltaDesc(T, N, Hk, Hv, Dk, Dv, dt, float(Dk) ** -0.5 if scale is None else float(scale), 0, 0, 0)
+
+
+def _delta_row(t, dtype, device, shape, name):
+    """Elements between the rows (t, n) of a [T, N, H, D] tensor whose rows are dense: a dense tensor's, or those of
+    a slice of a projection's output."""
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if t.device != device:
+        raise ValueError(f"{name} must be on {device}, got {t.device}")
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
+    T, N, H, D = shape
+    if t.is_contiguous():
+        return H * D
+    row = t.stride(1) if N > 1 else t.stride(0)
+    if (D > 1 and t.stride(3) != 1) or (H > 1 and t.stride(2) != D) or (T > 1 and t.stride(0) != N * row) or row < H * D:
+        raise ValueError(f"{name} of strides {t.stride()} must have dense rows [H, D] at equal distances")
+    return row
+
+
+def _delta_inputs(desc, q, k, v, g, beta, lengths, step=False):
+    """Checks the inputs; the descriptor with their row distances."""
+    if desc.dtype not in (MFPSN_F32, MFPSN_BF16):
+        raise TypeError("the delta rule is for f32 and bf16")
+    dev, st = q.device, STORAGE[desc.dtype]
+    T = 1 if step else desc.T
+    d = MfpsnDeltaDesc.from_buffer_copy(desc)
+    d.T = T
+    d.q_row = _delta_row(q, st, dev, (T, desc.N, desc.Hk, desc.Dk), "q")
+    d.k_row = _delta_row(k, st, dev, (T, desc.N, desc.Hk, desc.Dk), "k")
+    d.v_row = _delta_row(v, st, dev, (T, desc.N, desc.Hv, desc.Dv), "v")
+    for t, name in ((g, "g"), (beta, "beta")):
+        _shaped(t, st, dev, (T, desc.N, desc.Hv), name)
+    if lengths is not None:
+        _shaped(lengths, torch.int32, dev, (desc.N,), "lengths")
+    return d
+
+
+def _delta_state(desc, t, device, name):
+    if t is not None:
+        _shaped(t, torch.float32, device, (desc.N, desc.Hv, desc.Dk, desc.Dv), name)
+
+
+def delta_forward(desc: MfpsnDeltaDesc, q, k, v, g, beta, lengths=None, state=None, want_state: bool = False,
+                  want_saved: bool = False, workspace=None, stream=None):
+    """o [T, N, Hv, Dv], plus the state behind the sequences (want_state) and
+    what delta_backward needs (want_saved), in that order.  q, k, v may be
+    slices of one projection's output (rows [H, D] dense, at equal distances).
+    lengths: int32 [N] or None; state: float [N, Hv, Dk, Dv] or None (zeros)."""
+    dev = q.device
+    d = _delta_inputs(desc, q, k, v, g, beta, lengths)
+    _delta_state(desc, state, dev, "state")
+    guard, stream = _on(dev, stream)
+    with guard:
+        o = torch.empty((desc.T, desc.N, desc.Hv, desc.Dv), dtype=v.dtype, device=dev)
+        out = torch.empty((desc.N, desc.Hv, desc.Dk, desc.Dv), dtype=torch.float32, device=dev) if want_state else None
+        saved = None
+        if want_saved:
+            saved, workspace = torch.empty(max(mfpsn_delta_saved_size(d), 16), dtype=torch.uint8, device=dev), None
+        else:
+            need = mfpsn_delta_workspace_size(d)
+            if need and (workspace is None or _nbytes(workspace) < need):
+                workspace = torch.empty(need, dtype=torch.uint8, device=dev)
+        mfpsn_delta_forward(d, q, k, v, g, beta, lengths, state, o, out, saved, workspace, stream)
+    res = (o,) + ((out,) if want_state else ()) + ((saved,) if want_saved else ())
+    return res if len(res) > 1 else o
+
+
+def delta_backward(desc: MfpsnDeltaDesc, q, k, v, g, beta, saved, grad_o, lengths=None, grad_state=None,
+                   want_grad_state: bool = False, workspace=None, stream=None):
+    """grad_q, grad_k, grad_v, grad_g, grad_beta (and the gradient of the state
+    the forward began with) from the forward's saved.  grad_state: gradient of
+    the state behind the sequences, or None."""
+    dev = q.device
+    d = _delta_inputs(desc, q, k, v, g, beta, lengths)
+    _shaped(grad_o, v.dtype, dev, (desc.T, desc.N, desc.Hv, desc.Dv), "grad_o")
+    _delta_state(desc, grad_state, dev, "grad_state")
+    _expect(saved, torch.uint8, dev, "saved")
+    guard, stream = _on(dev, stream)
+    with guard:
+        grads = [torch.empty(t.shape, dtype=t.dtype, device=dev) for t in (q, k, v, g, beta)]
+        gs = torch.empty((desc.N, desc.Hv, desc.Dk, desc.Dv), dtype=torch.float32, device=dev) if want_grad_state else None
+        need = mfpsn_delta_backward_workspace_size(d)
+        if workspace is None or _nbytes(workspace) < need:
+            workspace = torch.empty(max(need, 16), dtype=torch.uint8, device=dev)
+        mfpsn_delta_backward(d, q, k, v, g, beta, lengths, saved, grad_o, grad_state, *grads, gs, workspace, stream)
+    return (*grads, gs) if want_grad_state else tuple(grads)
+
+
+def delta_step(desc: MfpsnDeltaDesc, q, k, v, g, beta, state, out=None, stream=None):
+    """One time step: q, k [1, N, Hk, Dk], v [1, N, Hv, Dv], g, beta
+    [1, N, Hv], state float [N, Hv, Dk, Dv] or None (zeros).  Returns o and the
+    new state, written into out = (o, state) if given (the state may be
+    updated in place); desc.T is ignored."""
+    dev = q.device
+    d = _delta_inputs(desc, q, k, v, g, beta, None, step=True)
+    _delta_state(desc, state, dev, "state")
+    guard, stream = _on(dev, stream)
+    with guard:
+        if out is None:
+            o = torch.empty((1, desc.N, desc.Hv, desc.Dv), dtype=v.dtype, device=dev)
+            new = torch.empty((desc.N, desc.Hv, desc.Dk, desc.Dv), dtype=torch.float32, device=dev)
+        else:
+            o, new = out
+            _shaped(o, v.dtype, dev, (1, desc.N, desc.Hv, desc.Dv), "o")
+            if new is None:
+                raise ValueError("out must hold o and the state")
+            _delta_state(desc, new, dev, "state")
+        mfpsn_delta_step(d, q, k, v, g, beta, state, o, new, stream)
+    return o, new
+
+
+class DeltaState:
+    """Step-by-step form of the gated delta rule: owns the states of N
+    sequences (float [N, Hv, Dk, Dv], zeros at first, or those that
+    delta_forward returned).  ``step`` takes one arriving time step of every
+    sequence and returns its outputs [N, Hv, Dv]; over a sequence this is what
+    ``delta_forward`` computes, up to rounding."""
+
+    def __init__(self, desc: MfpsnDeltaDesc, state=None, device="cuda"):
+        self.desc = desc
+        if state is None:
+            state = torch.zeros((desc.N, desc.Hv, desc.Dk, desc.Dv), dtype=torch.float32, device=device)
+        _delta_state(desc, state, state.device, "state")
+        self.state = state
+
+    def step(self, q, k, v, g, beta, stream=None, out=None):
+        """q, k [N, Hk, Dk], v [N, Hv, Dv], g, beta [N, Hv]."""
+        o = out if out is not None else torch.empty((self.desc.N, self.desc.Hv, self.desc.Dv), dtype=v.dtype,
+                                                    device=v.device)
+        delta_step(self.desc, q[None], k[None], v[None], g[None], beta[None], self.state, (o[None], self.state), stream)
+        return o
+
+
+class DeltaFunction(torch.autograd.Function):
+    """o, state_out = gated delta rule of q, k [T, N, Hk, Dk], v [T, N, Hv, Dv],
+    g, beta [T, N, Hv] (float32 or bfloat16, one type for all), scale (None:
+    1/sqrt(Dk)), state (float [N, Hv, Dk, Dv] or None) and lengths (int32 [N] or
+    None).  Gradients of all of them but scale and lengths."""
+
+    @staticmethod
+    def forward(ctx, q, k, v, g, beta, scale=None, state=None, lengths=None):
+        ins = [t.detach() for t in (q, k, v)] + [t.detach().contiguous() for t in (g, beta)]
+        st = state.detach().float().contiguous() if state is not None else None
+        desc = make_delta_desc(q.shape, v.shape, _float_dtype(v, "v"), scale)
+        o, out, saved = delta_forward(desc, *ins, lengths=lengths, state=st, want_state=True, want_saved=True)
+        ctx.save_for_backward(*ins, saved, lengths)
+        ctx.desc = desc
+        ctx.state_dtype = state.dtype if state is not None else None
+        ctx.set_materialize_grads(False)
+        return o, out
+
+    @staticmethod
+    def backward(ctx, grad_o, grad_state):
+        q, k, v, g, beta, saved, lengths = ctx.saved_tensors
+        if grad_o is None and grad_state is None:
+            return (None,) * 8
+        grad_o = torch.zeros(v.shape, dtype=v.dtype, device=v.device) if grad_o is None else grad_o.to(v.dtype).contiguous()
+        gs = grad_state.float().contiguous() if grad_state is not None else None
+        want = len(ctx.needs_input_grad) > 6 and ctx.needs_input_grad[6]
+        out = delta_backward(ctx.desc, q, k, v, g, beta, saved, grad_o, lengths, gs, want)
+        return (*out[:5], None, out[5].to(ctx.state_dtype) if want else None, None)
