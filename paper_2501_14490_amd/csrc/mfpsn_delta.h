@@ -49,7 +49,7 @@ struct DeltaLayout {
 };
 
 // Bytes of an element of P, U, S0 and dS: what the matrix products take
-constexpr bool kDeltaBf16Products = false;
+constexpr bool kDeltaBf16Products = true;
 inline int delta_elem(int dtype) { return kDeltaBf16Products && dtype == 1 ? 2 : 4; }
 
 inline int delta_dkp(int Dk) { return Dk <= 64 ? 64 : 128; }
