@@ -433,7 +433,8 @@ typedef struct mfpsn_delta_desc {
     int32_t Dk, Dv;  /* 1..128, 1..256                                             */
     int32_t dtype;   /* MFPSN_F32, MFPSN_BF16                                      */
     float scale;     /* of the outputs, finite                                     */
-    int64_t q_row, k_row, v_row; /* 0, or at least a row's Hk*Dk (Hv*Dv), < 2^40   */
+    int64_t q_row, k_row, v_row; /* 0, or at least a row's Hk*Dk (Hv*Dv); N rows   */
+                     /* of each stay below 2^30 elements                           */
 } mfpsn_delta_desc;
 
 int mfpsn_delta_workspace_size(const mfpsn_delta_desc* desc, size_t* bytes);

@@ -44,6 +44,12 @@ int validate_delta(const mfpsn_delta_desc* d)
         return MFPSN_ERR_SHAPE;
     if (!isfinite(d->scale))
         return MFPSN_ERR_PARAM;
+    // a time step of each tensor stays below 4 GiB (the kernels' 32-bit row distances)
+    const int64_t step = (((int64_t)1 << 32) - 1) / 4;
+    const int64_t rows[3] = {d->q_row ? d->q_row : qk, d->k_row ? d->k_row : qk, d->v_row > v ? d->v_row : v};
+    for (const int64_t r : rows)
+        if (d->N > 0 && r > step / d->N)
+            return MFPSN_ERR_SHAPE;
     // blocks of a launch: (sequence, head, chunk), (sequence, head, 32 columns)
     const int64_t nc = ((int64_t)d->T + kDeltaChunk - 1) / kDeltaChunk, heads = (int64_t)d->N * d->Hv;
     const int64_t each = nc > 8 ? nc : 8;
@@ -81,6 +87,11 @@ void fill(DeltaArgs& a, const mfpsn_delta_desc* d, const void* q, const void* k,
     a.k_row = d->k_row ? d->k_row : (int64_t)d->Hk * d->Dk;
     a.v_row = d->v_row ? d->v_row : (int64_t)d->Hv * d->Dv;
     const int es = elem_bytes(d->dtype);
+    a.q_step = (uint32_t)(a.q_row * a.N * es);
+    a.k_step = (uint32_t)(a.k_row * a.N * es);
+    a.v_step = (uint32_t)(a.v_row * a.N * es);
+    a.o_step = (uint32_t)((int64_t)a.N * a.Hv * a.Dv * es);
+    a.g_step = (uint32_t)((int64_t)a.N * a.Hv * es);
     a.vec_qk = wide_rows(q, a.q_row, d->Dk, es) && wide_rows(k, a.k_row, d->Dk, es);
     a.nc = (int32_t)(((int64_t)d->T + kDeltaChunk - 1) / kDeltaChunk);
     a.dvp = (d->Dv + 15) / 16 * 16;
@@ -307,7 +318,7 @@ int mfpsn_delta_backward(const mfpsn_delta_desc* desc, const void* q, const void
     fill(a, desc, q, k, v, g, beta, lengths);
     place(a, l, const_cast<void*>(saved), true);
     a.vec_v = wide_rows(grad_o, (int64_t)desc->Hv * desc->Dv, desc->Dv, es) &&
-              wide_rows(grad_v, (int64_t)desc->Hv * desc->Dv, desc->Dv, es);
+              wide_rows(grad_v, (int64_t)desc->Hv * desc->Dv, desc->Dv, es) && aligned(grad_q, 16) && aligned(grad_k, 16);
     a.grad_o = grad_o;
     a.grad_state_out = grad_state_out;
     a.dS = workspace;

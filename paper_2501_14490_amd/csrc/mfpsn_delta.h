@@ -19,7 +19,8 @@ struct DeltaArgs {
     int32_t T, N, Hk, Hv, Dk, Dv;
     float scale;
     int64_t q_row, k_row, v_row;  // elements between the rows of consecutive (t, n)
-    int32_t vec_qk, vec_v;        // rows of q and k (of v) may be read 16 bytes at a time
+    uint32_t q_step, k_step, v_step, o_step, g_step;  // bytes between consecutive t (o: grad_o and grad_v too)
+    int32_t vec_qk, vec_v;        // rows of q and k (of the gradients) may be read and written 16 bytes at a time
     int32_t nc;                   // chunks of the longest sequence
     int32_t dvp;                  // Dv rounded up to 16
     const void *q, *k, *v, *g, *beta;
@@ -49,8 +50,7 @@ struct DeltaLayout {
 };
 
 // Bytes of an element of P, U, S0 and dS: what the matrix products take
-constexpr bool kDeltaBf16Products = true;
-inline int delta_elem(int dtype) { return kDeltaBf16Products && dtype == 1 ? 2 : 4; }
+inline int delta_elem(int dtype) { return dtype == 1 ? 2 : 4; }
 
 inline int delta_dkp(int Dk) { return Dk <= 64 ? 64 : 128; }
 

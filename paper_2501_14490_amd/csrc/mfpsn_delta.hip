@@ -131,22 +131,28 @@ __device__ void unit_lower_inverse(const float* A, float* X)
 }
 
 // X, P and the gates of a chunk, for the value heads of one key head
-template <typename D, bool BF, int DKP> struct PrepLds {
+template <bool BF, int DKP> struct PrepLds {
     using El = typename Mat<BF>::El;
     static constexpr int LDK = DKP + Mat<BF>::PAD;
-    El k[L * LDK], q[L * LDK];
-    float A[L * LF], X[L * LF];
+    union {
+        struct {
+            El k[L * LDK], q[L * LDK];
+        };
+        struct {  // (once the products of k and q are in registers)
+            float A[L * LF], X[L * LF];
+        };
+    };
     double G[L];
     float beta[L];
 };
 
-template <typename D, bool BF, int DKP>
+template <typename D, bool BF, int DKP, bool VEC>
 __global__ __launch_bounds__(256) void delta_prep(DeltaArgs a)
 {
     using T = typename D::T;
     using M = Mat<BF>;
     using El = typename M::El;
-    using Lds = PrepLds<D, BF, DKP>;
+    using Lds = PrepLds<BF, DKP>;
     __shared__ Lds s;
     const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, col = lane & 15, g4 = 4 * (lane >> 4);
     const int c = blockIdx.x % a.nc;
@@ -156,10 +162,13 @@ __global__ __launch_bounds__(256) void delta_prep(DeltaArgs a)
     if (live <= 0)
         return;
     const int64_t row0 = (int64_t)t0 * a.N + n;
-    stage<D, El, DKP, 256>(s.k, Lds::LDK, (const T*)a.k + row0 * a.k_row + (int64_t)hk * a.Dk, (int64_t)a.N * a.k_row, live,
-                           a.Dk, a.vec_qk);
-    stage<D, El, DKP, 256>(s.q, Lds::LDK, (const T*)a.q + row0 * a.q_row + (int64_t)hk * a.Dk, (int64_t)a.N * a.q_row, live,
-                           a.Dk, a.vec_qk);
+    {
+        Rows<D, El, DKP, 256, VEC> k, q;
+        k.load((const T*)a.k + row0 * a.k_row + (int64_t)hk * a.Dk, a.k_step, live, a.Dk);
+        q.load((const T*)a.q + row0 * a.q_row + (int64_t)hk * a.Dk, a.q_step, live, a.Dk);
+        k.store(s.k, Lds::LDK, live, a.Dk);
+        q.store(s.q, Lds::LDK, live, a.Dk);
+    }
     __syncthreads();
     // (K K^T)[j][i] and (K Q^T)[j][i]: column i = 16 wave + col of every row tile j <= i
     f32x4 kk[4], kq[4];
@@ -178,6 +187,7 @@ __global__ __launch_bounds__(256) void delta_prep(DeltaArgs a)
                 kq[t] = M::mma(ak, bq, kq[t]);
             }
     }
+    __syncthreads();
     const int i = 16 * wave + col;
     for (int r = 0; r < group; ++r) {
         const int hv = hk * group + r;
@@ -209,14 +219,7 @@ __global__ __launch_bounds__(256) void delta_prep(DeltaArgs a)
                     }
                 }
             *(f32x4*)(s.A + i * LF + j0) = av;
-            alignas(16) El e4[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-                e4[e] = M::put(pv[e]);
-            if constexpr (BF)
-                *(uint2*)(P + i * L + j0) = *(const uint2*)e4;
-            else
-                *(uint4*)(P + i * L + j0) = *(const uint4*)e4;
+            put4<BF>(P + i * L + j0, pv);
         }
         __syncthreads();
         unit_lower_inverse(s.A, s.X);
@@ -245,32 +248,36 @@ __global__ __launch_bounds__(256) void delta_prep(DeltaArgs a)
 // of the state, all Dk rows, in registers, and everything that is computed from
 // them: residuals, outputs and the state itself go from product to product
 // without leaving the wave.  The block's waves share the chunk's K, Q, X and P
-// in LDS.
-template <typename D, bool BF, int DKP> struct ScanLds {
+// in LDS; the next chunk's are on their way into registers meanwhile.  One wave
+// a SIMD (the state, the operands of the next products and the next tiles
+// take more than half of the registers), so nothing but the order of its own
+// instructions hides a wave's latencies: operands are read a group ahead.
+template <bool BF, int DKP> struct ScanLds {
     using El = typename Mat<BF>::El;
     static constexpr int LDK = DKP + Mat<BF>::PAD, LDL = L + Mat<BF>::PAD;
     El k[L * LDK], q[L * LDK];
     El x[BF ? 2 : 1][L * LDL], p[L * LDL];
-    float gate[2][L], beta[L];
+    float gate[2 * L], beta[L];
 };
 
-template <typename D, bool BF, int DKP, int NW>
-__global__ __launch_bounds__(NW * 64) void delta_scan(DeltaArgs a)
+template <typename D, bool BF, int DKP, int NW, bool VEC>
+__global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(1, 1))) void delta_scan(DeltaArgs a)
 {
     using T = typename D::T;
     using M = Mat<BF>;
     using El = typename M::El;
     using Frag = typename M::Frag;
-    using Lds = ScanLds<D, BF, DKP>;
-    constexpr int TK = DKP / 16, TH = NW * 64, KU = M::KU, TU = M::TU, UL = L / KU;
+    using Lds = ScanLds<BF, DKP>;
+    constexpr int TK = DKP / 16, TH = NW * 64, KU = M::KU, TU = M::TU, UK = DKP / KU, UL = L / KU;
+    static_assert(TH >= 2 * L);
     __shared__ Lds s;
     const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, col = lane & 15, g4 = 4 * (lane >> 4);
     const int vblocks = (a.dvp + 16 * NW - 1) / (16 * NW);
     const int64_t head = blockIdx.x / vblocks;
     const int n = (int)(head / a.Hv), hv = (int)(head - (int64_t)n * a.Hv), hk = hv / (a.Hv / a.Hk);
     const int v = ((int)(blockIdx.x % vblocks) * NW + wave) * 16 + col;
-    const bool mine = v < a.Dv;          // a column of the tensors
-    const bool wide = v - col < a.dvp;   // the wave has columns of the padded arrays
+    const bool mine = v < a.Dv;         // a column of the tensors
+    const bool wide = v - col < a.dvp;  // the wave has columns of the padded arrays
     const int len = length_of(a, n), chunks = (len + L - 1) / L;
     f32x4 S[TK];
 #pragma unroll
@@ -280,75 +287,129 @@ __global__ __launch_bounds__(NW * 64) void delta_scan(DeltaArgs a)
             const int d = 16 * t + g4 + r;
             S[t][r] = a.state_in && mine && d < a.Dk ? a.state_in[(head * a.Dk + d) * a.Dv + v] : 0.0f;
         }
+    Rows<D, El, DKP, TH, VEC> nk, nq;
+    Dense<El, L, L, TH> nx[BF ? 2 : 1], np;
+    T nv[16];
+    float ngate = 0.0f, nbeta = 0.0f;
+    const auto fetch = [&](int c) {
+        const int t0 = c * L, live = min(L, len - t0);
+        const int64_t row0 = (int64_t)t0 * a.N + n, unit = unit_of(a, n, hv, c);
+        nk.load((const T*)a.k + row0 * a.k_row + (int64_t)hk * a.Dk, a.k_step, live, a.Dk);
+        nq.load((const T*)a.q + row0 * a.q_row + (int64_t)hk * a.Dk, a.q_step, live, a.Dk);
+        nx[0].load((const El*)a.X + unit * L * L * (BF ? 2 : 1));
+        if constexpr (BF)
+            nx[1].load((const El*)a.X + unit * L * L * 2 + L * L);
+        np.load((const El*)a.P + unit * L * L);
+        const T* pv = (const T*)a.v + row0 * a.v_row + (int64_t)hv * a.Dv + (mine ? v : 0);
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+            nv[e] = *row_at(pv, min(16 * (e >> 2) + g4 + (e & 3), live - 1), a.v_step);
+        if (tid < 2 * L)
+            ngate = a.gate[unit * 2 * L + tid];
+        if (tid < L)
+            nbeta = D::get(*row_at((const T*)a.beta + row0 * a.Hv + hv, min(tid, live - 1), a.g_step));
+    };
+    if (chunks > 0)
+        fetch(0);
     for (int c = 0; c < chunks; ++c) {
         const int t0 = c * L, live = min(L, len - t0);
         const int64_t row0 = (int64_t)t0 * a.N + n, unit = unit_of(a, n, hv, c);
         __syncthreads();
-        stage<D, El, DKP, TH>(s.k, Lds::LDK, (const T*)a.k + row0 * a.k_row + (int64_t)hk * a.Dk, (int64_t)a.N * a.k_row,
-                              live, a.Dk, a.vec_qk);
-        stage<D, El, DKP, TH>(s.q, Lds::LDK, (const T*)a.q + row0 * a.q_row + (int64_t)hk * a.Dk, (int64_t)a.N * a.q_row,
-                              live, a.Dk, a.vec_qk);
-        stage_dense<El, L, L, TH>(s.x[0], Lds::LDL, (const El*)a.X + unit * L * L * (BF ? 2 : 1));
+        nk.store(s.k, Lds::LDK, live, a.Dk);
+        nq.store(s.q, Lds::LDK, live, a.Dk);
+        nx[0].store(s.x[0], Lds::LDL);
         if constexpr (BF)
-            stage_dense<El, L, L, TH>(s.x[1], Lds::LDL, (const El*)a.X + unit * L * L * 2 + L * L);
-        stage_dense<El, L, L, TH>(s.p, Lds::LDL, (const El*)a.P + unit * L * L);
-        for (int i = tid; i < L; i += TH) {
-            s.gate[0][i] = a.gate[unit * 2 * L + i];
-            s.gate[1][i] = a.gate[unit * 2 * L + L + i];
-            s.beta[i] = i < live ? D::get(((const T*)a.beta)[(row0 + (int64_t)i * a.N) * a.Hv + hv]) : 0.0f;
-        }
+            nx[1].store(s.x[1], Lds::LDL);
+        np.store(s.p, Lds::LDL);
+        if (tid < 2 * L)
+            s.gate[tid] = ngate;
+        if (tid < L)
+            s.beta[tid] = tid < live ? nbeta : 0.0f;
         f32x4 R[4];
 #pragma unroll
         for (int t = 0; t < 4; ++t)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int i = 16 * t + g4 + r;
-                R[t][r] = mine && i < live ? D::get(((const T*)a.v)[(row0 + (int64_t)i * a.N) * a.v_row + (int64_t)hv * a.Dv + v])
-                                           : 0.0f;
-            }
+            for (int r = 0; r < 4; ++r)
+                R[t][r] = mine && 16 * t + g4 + r < live ? D::get(nv[4 * t + r]) : 0.0f;
         __syncthreads();
+        if (c + 1 < chunks)
+            fetch(c + 1);
         if (a.S0 && wide) {  // [v][d], for the backward
             El* S0 = (El*)a.S0 + (unit * a.dvp + v) * DKP;
 #pragma unroll
             for (int t = 0; t < TK; ++t)
-#pragma unroll
-                for (int r = 0; r < 4; ++r)
-                    S0[16 * t + g4 + r] = M::put(S[t][r]);
+                put4<BF>(S0 + 16 * t + g4, S[t]);
         }
-        // K S0 and Q S0.  16-bit: the state goes in as two numbers of 8 bits each for the residuals (they
-        // make the next state, which is kept in float), as one for the outputs (rounded to 8 bits anyway).
-        f32x4 KS[4], O[4];
+        // K S0 and Q S0.  16-bit: the state goes in as the sum of two numbers of 8 bits each.
+        f32x4 KS[4], O[4], eG[4], to_end[4];
+        Frag fk[2][4], fq[2][4], fx[UL][4], fl[UL][4], fp[UL][4], ft[2][TK];
+        const auto read_kq = [&](int u) {
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+                fk[u & 1][t] = M::rows(s.k + 16 * t * Lds::LDK, Lds::LDK, u);
+                fq[u & 1][t] = M::rows(s.q + 16 * t * Lds::LDK, Lds::LDK, u);
+            }
+        };
 #pragma unroll
         for (int t = 0; t < 4; ++t)
             KS[t] = O[t] = f32x4{0, 0, 0, 0};
+        read_kq(0);
+        in_order();
 #pragma unroll
-        for (int u = 0; u < DKP / KU; ++u) {
+        for (int u = 0; u < UK; ++u) {
+            if (u + 1 < UK) {
+                read_kq(u + 1);
+            } else {
+#pragma unroll
+                for (int t = 0; t < 4; ++t) {
+                    eG[t] = *(const f32x4*)(s.gate + 16 * t + g4);
+                    to_end[t] = *(const f32x4*)(s.gate + L + 16 * t + g4) * *(const f32x4*)(s.beta + 16 * t + g4);
+                }
+#pragma unroll
+                for (int w = 0; w < UL; ++w)
+#pragma unroll
+                    for (int t = 0; t < 4; ++t)
+                        if (w * KU < 16 * (t + 1)) {  // (X and P are lower triangular)
+                            fx[w][t] = M::rows(s.x[0] + 16 * t * Lds::LDL, Lds::LDL, w);
+                            if constexpr (BF)
+                                fl[w][t] = M::rows(s.x[1] + 16 * t * Lds::LDL, Lds::LDL, w);
+                        }
+            }
+            in_order();
             const Frag b = M::pack(S + u * TU);
-            Frag rest;
-            if constexpr (BF)
-                rest = M::pack_rest(S + u * TU, b);
 #pragma unroll
             for (int t = 0; t < 4; ++t) {
-                const Frag ak = M::rows(s.k + 16 * t * Lds::LDK, Lds::LDK, u);
-                KS[t] = M::mma(ak, b, KS[t]);
-                if constexpr (BF)
-                    KS[t] = M::mma(ak, rest, KS[t]);
-                O[t] = M::mma(M::rows(s.q + 16 * t * Lds::LDK, Lds::LDK, u), b, O[t]);
+                KS[t] = M::mma(fk[u & 1][t], b, KS[t]);
+                O[t] = M::mma(fq[u & 1][t], b, O[t]);
             }
-        }
-        f32x4 eG[4];
+            if constexpr (BF) {
+                const Frag rest = M::pack_rest(S + u * TU, b);
 #pragma unroll
-        for (int t = 0; t < 4; ++t) {
-            eG[t] = *(const f32x4*)(s.gate[0] + 16 * t + g4);
-#pragma unroll
-            for (int r = 0; r < 4; ++r)
-                R[t][r] = __builtin_fmaf(-eG[t][r], KS[t][r], R[t][r]);
+                for (int t = 0; t < 4; ++t) {
+                    KS[t] = M::mma(fk[u & 1][t], rest, KS[t]);
+                    O[t] = M::mma(fq[u & 1][t], rest, O[t]);
+                }
+            }
+            in_order();
         }
-        // residuals r = X R (X is lower triangular)
+#pragma unroll
+        for (int w = 0; w < UL; ++w)
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+                if (w * KU < 16 * (t + 1))
+                    fp[w][t] = M::rows(s.p + 16 * t * Lds::LDL, Lds::LDL, w);
+        in_order();
+        // residuals r = X (V - diag(e^G) K S0)
         f32x4 U[4];
 #pragma unroll
-        for (int t = 0; t < 4; ++t)
+        for (int t = 0; t < 4; ++t) {
             U[t] = f32x4{0, 0, 0, 0};
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                R[t][r] = __builtin_fmaf(-eG[t][r], KS[t][r], R[t][r]);
+                O[t][r] *= a.scale * eG[t][r];
+            }
+        }
 #pragma unroll
         for (int u = 0; u < UL; ++u) {
             const Frag b = M::pack(R + u * TU);
@@ -358,53 +419,50 @@ __global__ __launch_bounds__(NW * 64) void delta_scan(DeltaArgs a)
 #pragma unroll
             for (int t = 0; t < 4; ++t)
                 if (u * KU < 16 * (t + 1)) {
-                    const Frag ax = M::rows(s.x[0] + 16 * t * Lds::LDL, Lds::LDL, u);
-                    U[t] = M::mma(ax, b, U[t]);
+                    U[t] = M::mma(fx[u][t], b, U[t]);
                     if constexpr (BF) {
-                        U[t] = M::mma(ax, rest, U[t]);
-                        U[t] = M::mma(M::rows(s.x[1] + 16 * t * Lds::LDL, Lds::LDL, u), b, U[t]);
+                        U[t] = M::mma(fx[u][t], rest, U[t]);
+                        U[t] = M::mma(fl[u][t], b, U[t]);
                     }
                 }
         }
+        const auto read_kt = [&](int u) {
+#pragma unroll
+            for (int t = 0; t < TK; ++t)
+                ft[u & 1][t] = M::cols(s.k + 16 * t, Lds::LDK, u);
+        };
+        in_order();
+        read_kt(0);
+        in_order();
         if (a.U && wide) {  // [v][i]
             El* pu = (El*)a.U + (unit * a.dvp + v) * L;
 #pragma unroll
             for (int t = 0; t < 4; ++t)
-#pragma unroll
-                for (int r = 0; r < 4; ++r)
-                    pu[16 * t + g4 + r] = M::put(U[t][r]);
+                put4<BF>(pu + 16 * t + g4, U[t]);
         }
         // outputs
-#pragma unroll
-        for (int t = 0; t < 4; ++t)
-#pragma unroll
-            for (int r = 0; r < 4; ++r)
-                O[t][r] *= a.scale * eG[t][r];
 #pragma unroll
         for (int u = 0; u < UL; ++u) {
             const Frag b = M::pack(U + u * TU);
 #pragma unroll
             for (int t = 0; t < 4; ++t)
                 if (u * KU < 16 * (t + 1))
-                    O[t] = M::mma(M::rows(s.p + 16 * t * Lds::LDL, Lds::LDL, u), b, O[t]);
+                    O[t] = M::mma(fp[u][t], b, O[t]);
+            if constexpr (BF) {
+                const Frag rest = M::pack_rest(U + u * TU, b);
+#pragma unroll
+                for (int t = 0; t < 4; ++t)
+                    if (u * KU < 16 * (t + 1))
+                        O[t] = M::mma(fp[u][t], rest, O[t]);
+            }
         }
+        // the state behind the chunk
+        const float last = s.gate[L - 1];
 #pragma unroll
         for (int t = 0; t < 4; ++t)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int i = 16 * t + g4 + r;
-                if (mine && i < live)
-                    ((T*)a.o)[((row0 + (int64_t)i * a.N) * a.Hv + hv) * a.Dv + v] = D::put(O[t][r]);
-            }
-        // the state behind the chunk
-        const float last = s.gate[0][L - 1];
-#pragma unroll
-        for (int t = 0; t < 4; ++t) {
-            const f32x4 e = *(const f32x4*)(s.gate[1] + 16 * t + g4), b = *(const f32x4*)(s.beta + 16 * t + g4);
-#pragma unroll
             for (int r = 0; r < 4; ++r)
-                U[t][r] *= e[r] * b[r];
-        }
+                U[t][r] *= to_end[t][r];
 #pragma unroll
         for (int t = 0; t < TK; ++t)
 #pragma unroll
@@ -412,18 +470,30 @@ __global__ __launch_bounds__(NW * 64) void delta_scan(DeltaArgs a)
                 S[t][r] *= last;
 #pragma unroll
         for (int u = 0; u < UL; ++u) {
+            if (u + 1 < UL)
+                read_kt(u + 1);
+            in_order();
             const Frag b = M::pack(U + u * TU);
-            Frag rest;
-            if constexpr (BF)
-                rest = M::pack_rest(U + u * TU, b);
 #pragma unroll
-            for (int t = 0; t < TK; ++t) {
-                const Frag ak = M::cols(s.k + 16 * t, Lds::LDK, u);
-                S[t] = M::mma(ak, b, S[t]);
-                if constexpr (BF)
-                    S[t] = M::mma(ak, rest, S[t]);
+            for (int t = 0; t < TK; ++t)
+                S[t] = M::mma(ft[u & 1][t], b, S[t]);
+            if constexpr (BF) {
+                const Frag rest = M::pack_rest(U + u * TU, b);
+#pragma unroll
+                for (int t = 0; t < TK; ++t)
+                    S[t] = M::mma(ft[u & 1][t], rest, S[t]);
             }
+            in_order();
         }
+        T* po = (T*)a.o + (row0 * a.Hv + hv) * a.Dv + v;
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int i = 16 * t + g4 + r;
+                if (mine && i < live)
+                    *const_cast<T*>(row_at(po, i, a.o_step)) = D::put(O[t][r]);
+            }
     }
     if (!mine)
         return;
@@ -440,23 +510,25 @@ __global__ __launch_bounds__(NW * 64) void delta_scan(DeltaArgs a)
             }
 }
 
-// The chunks in reverse: the gradient of the state, the values' gradient
-template <typename D, bool BF, int DKP> struct RscanLds {
+// The chunks in reverse, in the same manner: the gradient of the state, the
+// values' gradient
+template <bool BF, int DKP> struct RscanLds {
     using El = typename Mat<BF>::El;
     static constexpr int LDK = DKP + Mat<BF>::PAD, LDL = L + Mat<BF>::PAD;
     El k[L * LDK], q[L * LDK], x[L * LDL], p[L * LDL];
-    float gate[2][L], beta[L];
+    float gate[2 * L], beta[L];
 };
 
-template <typename D, bool BF, int DKP, int NW>
-__global__ __launch_bounds__(NW * 64) void delta_rscan(DeltaArgs a)
+template <typename D, bool BF, int DKP, int NW, bool VEC>
+__global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(1, 1))) void delta_rscan(DeltaArgs a)
 {
     using T = typename D::T;
     using M = Mat<BF>;
     using El = typename M::El;
     using Frag = typename M::Frag;
-    using Lds = RscanLds<D, BF, DKP>;
-    constexpr int TK = DKP / 16, TH = NW * 64, KU = M::KU, TU = M::TU, UL = L / KU;
+    using Lds = RscanLds<BF, DKP>;
+    constexpr int TK = DKP / 16, TH = NW * 64, KU = M::KU, TU = M::TU, UK = DKP / KU, UL = L / KU;
+    static_assert(TH >= 2 * L);
     __shared__ Lds s;
     const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, col = lane & 15, g4 = 4 * (lane >> 4);
     const int vblocks = (a.dvp + 16 * NW - 1) / (16 * NW);
@@ -473,93 +545,128 @@ __global__ __launch_bounds__(NW * 64) void delta_rscan(DeltaArgs a)
             const int d = 16 * t + g4 + r;
             S[t][r] = a.grad_state_out && mine && d < a.Dk ? a.grad_state_out[(head * a.Dk + d) * a.Dv + v] : 0.0f;
         }
+    Rows<D, El, DKP, TH, VEC> nk, nq;
+    Dense<El, L, L, TH> nx, np;
+    T no[16];
+    float ngate = 0.0f, nbeta = 0.0f;
+    const auto fetch = [&](int c) {
+        const int t0 = c * L, live = min(L, len - t0);
+        const int64_t row0 = (int64_t)t0 * a.N + n, unit = unit_of(a, n, hv, c);
+        nk.load((const T*)a.k + row0 * a.k_row + (int64_t)hk * a.Dk, a.k_step, live, a.Dk);
+        nq.load((const T*)a.q + row0 * a.q_row + (int64_t)hk * a.Dk, a.q_step, live, a.Dk);
+        nx.load((const El*)a.X + unit * L * L * (BF ? 2 : 1));
+        np.load((const El*)a.P + unit * L * L);
+        const T* po = (const T*)a.grad_o + (row0 * a.Hv + hv) * a.Dv + (mine ? v : 0);
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+            no[e] = *row_at(po, min(16 * (e >> 2) + g4 + (e & 3), live - 1), a.o_step);
+        if (tid < 2 * L)
+            ngate = a.gate[unit * 2 * L + tid];
+        if (tid < L)
+            nbeta = D::get(*row_at((const T*)a.beta + row0 * a.Hv + hv, min(tid, live - 1), a.g_step));
+    };
+    if (chunks > 0)
+        fetch(chunks - 1);
     for (int c = chunks - 1; c >= 0; --c) {
         const int t0 = c * L, live = min(L, len - t0);
         const int64_t row0 = (int64_t)t0 * a.N + n, unit = unit_of(a, n, hv, c);
         __syncthreads();
-        stage<D, El, DKP, TH>(s.k, Lds::LDK, (const T*)a.k + row0 * a.k_row + (int64_t)hk * a.Dk, (int64_t)a.N * a.k_row,
-                              live, a.Dk, a.vec_qk);
-        stage<D, El, DKP, TH>(s.q, Lds::LDK, (const T*)a.q + row0 * a.q_row + (int64_t)hk * a.Dk, (int64_t)a.N * a.q_row,
-                              live, a.Dk, a.vec_qk);
-        stage_dense<El, L, L, TH>(s.x, Lds::LDL, (const El*)a.X + unit * L * L * (BF ? 2 : 1));
-        stage_dense<El, L, L, TH>(s.p, Lds::LDL, (const El*)a.P + unit * L * L);
-        for (int i = tid; i < L; i += TH) {
-            s.gate[0][i] = a.gate[unit * 2 * L + i];
-            s.gate[1][i] = a.gate[unit * 2 * L + L + i];
-            s.beta[i] = i < live ? D::get(((const T*)a.beta)[(row0 + (int64_t)i * a.N) * a.Hv + hv]) : 0.0f;
-        }
+        nk.store(s.k, Lds::LDK, live, a.Dk);
+        nq.store(s.q, Lds::LDK, live, a.Dk);
+        nx.store(s.x, Lds::LDL);
+        np.store(s.p, Lds::LDL);
+        if (tid < 2 * L)
+            s.gate[tid] = ngate;
+        if (tid < L)
+            s.beta[tid] = tid < live ? nbeta : 0.0f;
         f32x4 dO[4];
 #pragma unroll
         for (int t = 0; t < 4; ++t)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int i = 16 * t + g4 + r;
-                dO[t][r] = mine && i < live ? D::get(((const T*)a.grad_o)[((row0 + (int64_t)i * a.N) * a.Hv + hv) * a.Dv + v])
-                                            : 0.0f;
-            }
+            for (int r = 0; r < 4; ++r)
+                dO[t][r] = mine && 16 * t + g4 + r < live ? D::get(no[4 * t + r]) : 0.0f;
         __syncthreads();
+        if (c > 0)
+            fetch(c - 1);
         if (wide) {  // [v][d], for delta_grads
             El* dS = (El*)a.dS + (unit * a.dvp + v) * DKP;
 #pragma unroll
             for (int t = 0; t < TK; ++t)
-#pragma unroll
-                for (int r = 0; r < 4; ++r)
-                    dS[16 * t + g4 + r] = M::put(S[t][r]);
+                put4<BF>(dS + 16 * t + g4, S[t]);
         }
         // dr' = diag(e^{G_last - G} beta) K dS1 + P^T dO
-        f32x4 R[4];
+        f32x4 R[4], eG[4], to_end[4];
+        Frag fk[2][4], fp[UL][4], fx[UL][4], ft[2][TK];
+        const auto read_k = [&](int u) {
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+                fk[u & 1][t] = M::rows(s.k + 16 * t * Lds::LDK, Lds::LDK, u);
+        };
 #pragma unroll
         for (int t = 0; t < 4; ++t)
             R[t] = f32x4{0, 0, 0, 0};
+        read_k(0);
+        in_order();
 #pragma unroll
-        for (int u = 0; u < DKP / KU; ++u) {
+        for (int u = 0; u < UK; ++u) {
+            if (u + 1 < UK) {
+                read_k(u + 1);
+            } else {
+#pragma unroll
+                for (int t = 0; t < 4; ++t) {
+                    eG[t] = *(const f32x4*)(s.gate + 16 * t + g4);
+                    to_end[t] = *(const f32x4*)(s.gate + L + 16 * t + g4) * *(const f32x4*)(s.beta + 16 * t + g4);
+                }
+#pragma unroll
+                for (int w = 0; w < UL; ++w)
+#pragma unroll
+                    for (int t = 0; t < 4; ++t)
+                        if ((w + 1) * KU > 16 * t)  // (transposed: upper triangular)
+                            fp[w][t] = M::cols(s.p + 16 * t, Lds::LDL, w);
+            }
+            in_order();
             const Frag b = M::pack(S + u * TU);
 #pragma unroll
             for (int t = 0; t < 4; ++t)
-                R[t] = M::mma(M::rows(s.k + 16 * t * Lds::LDK, Lds::LDK, u), b, R[t]);
+                R[t] = M::mma(fk[u & 1][t], b, R[t]);
+            in_order();
         }
 #pragma unroll
-        for (int t = 0; t < 4; ++t) {
-            const f32x4 e = *(const f32x4*)(s.gate[1] + 16 * t + g4), b = *(const f32x4*)(s.beta + 16 * t + g4);
+        for (int w = 0; w < UL; ++w)
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+                if ((w + 1) * KU > 16 * t)
+                    fx[w][t] = M::cols(s.x + 16 * t, Lds::LDL, w);
+        const auto read_t = [&](const El* tile, int u) {
+#pragma unroll
+            for (int t = 0; t < TK; ++t)
+                ft[u & 1][t] = M::cols(tile + 16 * t, Lds::LDK, u);
+        };
+        read_t(s.q, 0);
+        in_order();
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
 #pragma unroll
             for (int r = 0; r < 4; ++r)
-                R[t][r] *= e[r] * b[r];
-        }
+                R[t][r] *= to_end[t][r];
 #pragma unroll
         for (int u = 0; u < UL; ++u) {
             const Frag b = M::pack(dO + u * TU);
 #pragma unroll
             for (int t = 0; t < 4; ++t)
                 if ((u + 1) * KU > 16 * t)
-                    R[t] = M::mma(M::cols(s.p + 16 * t, Lds::LDL, u), b, R[t]);
+                    R[t] = M::mma(fp[u][t], b, R[t]);
         }
-        // dV = X^T dr'
+        // dV = X^T dr', and meanwhile dS0 = e^{G_last} dS1 + scale Q^T diag(e^G) dO - K^T diag(e^G) dV
         f32x4 dV[4];
-#pragma unroll
-        for (int t = 0; t < 4; ++t)
-            dV[t] = f32x4{0, 0, 0, 0};
-#pragma unroll
-        for (int u = 0; u < UL; ++u) {
-            const Frag b = M::pack(R + u * TU);
-#pragma unroll
-            for (int t = 0; t < 4; ++t)
-                if ((u + 1) * KU > 16 * t)
-                    dV[t] = M::mma(M::cols(s.x + 16 * t, Lds::LDL, u), b, dV[t]);
-        }
-        const float last = s.gate[0][L - 1];
+        const float last = s.gate[L - 1];
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
-            const f32x4 eG = *(const f32x4*)(s.gate[0] + 16 * t + g4);
+            dV[t] = f32x4{0, 0, 0, 0};
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int i = 16 * t + g4 + r;
-                if (mine && i < live)
-                    ((T*)a.grad_v)[((row0 + (int64_t)i * a.N) * a.Hv + hv) * a.Dv + v] = D::put(dV[t][r]);
-                dO[t][r] *= a.scale * eG[r];
-                dV[t][r] *= -eG[r];
-            }
+            for (int r = 0; r < 4; ++r)
+                dO[t][r] *= a.scale * eG[t][r];
         }
-        // dS0
 #pragma unroll
         for (int t = 0; t < TK; ++t)
 #pragma unroll
@@ -567,12 +674,45 @@ __global__ __launch_bounds__(NW * 64) void delta_rscan(DeltaArgs a)
                 S[t][r] *= last;
 #pragma unroll
         for (int u = 0; u < UL; ++u) {
-            const Frag bo = M::pack(dO + u * TU), bv = M::pack(dV + u * TU);
+            if (u + 1 < UL)
+                read_t(s.q, u + 1);
+            in_order();
+            const Frag b = M::pack(dO + u * TU);
 #pragma unroll
-            for (int t = 0; t < TK; ++t) {
-                S[t] = M::mma(M::cols(s.q + 16 * t, Lds::LDK, u), bo, S[t]);
-                S[t] = M::mma(M::cols(s.k + 16 * t, Lds::LDK, u), bv, S[t]);
+            for (int t = 0; t < TK; ++t)
+                S[t] = M::mma(ft[u & 1][t], b, S[t]);
+            in_order();
+        }
+        read_t(s.k, 0);
+        in_order();
+#pragma unroll
+        for (int u = 0; u < UL; ++u) {
+            const Frag b = M::pack(R + u * TU);
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+                if ((u + 1) * KU > 16 * t)
+                    dV[t] = M::mma(fx[u][t], b, dV[t]);
+        }
+        T* pv = (T*)a.grad_v + (row0 * a.Hv + hv) * a.Dv + v;
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int i = 16 * t + g4 + r;
+                if (mine && i < live)
+                    *const_cast<T*>(row_at(pv, i, a.o_step)) = D::put(dV[t][r]);
+                dV[t][r] *= -eG[t][r];
             }
+#pragma unroll
+        for (int u = 0; u < UL; ++u) {
+            if (u + 1 < UL)
+                read_t(s.k, u + 1);
+            in_order();
+            const Frag b = M::pack(dV + u * TU);
+#pragma unroll
+            for (int t = 0; t < TK; ++t)
+                S[t] = M::mma(ft[u & 1][t], b, S[t]);
+            in_order();
         }
     }
     if (!mine)
@@ -591,10 +731,12 @@ __global__ __launch_bounds__(NW * 64) void delta_rscan(DeltaArgs a)
 }
 
 // The gradients of a chunk's queries, keys, decays and write strengths, for
-// one key head.  All products are computed transposed: wave w has the columns
-// i = 16 w .. 16 w + 15 (steps) of every result, so a step's factors are one
-// value a lane, and E^T, F^T in registers are the right operands of E K, F K.
-template <typename D, bool BF, int DKP> struct GradsLds {
+// one key head.  All products are computed transposed: waves w and w + 4 have
+// the columns i = 16 w .. 16 w + 15 (steps) of every result, so a step's
+// factors are one value a lane; each of the two has half of the keys' rows,
+// and one of the matrices E, F that the products of the second part share
+// through LDS.  8 waves, two a SIMD.
+template <bool BF, int DKP> struct GradsLds {
     using El = typename Mat<BF>::El;
     static constexpr int VB = BF ? 64 : 32;  // values staged at a time
     static constexpr int LDK = DKP + Mat<BF>::PAD, LDL = L + Mat<BF>::PAD, LDV = VB + Mat<BF>::PAD;
@@ -603,204 +745,248 @@ template <typename D, bool BF, int DKP> struct GradsLds {
         struct {
             El dO[L * LDV], dV[L * LDV], r[VB * LDL], S0[VB * LDK], dS[VB * LDK];
         } v;
-        struct {
-            El E[L * LDL], F[L * LDL];  // [i][j]
-        } m;
+        El EF[2][L * LDL];  // [i][j]
     };
     double G[L];
     float eG[L], to_end[L], beta[L];
-    float sum[4][L];           // over a wave's steps i, of each step j
-    float a[L], x[L], row[L];  // of each step
-    float z[4];
+    float sum[8][L];                             // over a wave's steps i > j, of each step j
+    float a[2][L], x[2][L], row[2][L], diag[L];  // of each step
+    float z[8];
 };
 
-template <typename D, bool BF, int DKP>
-__global__ __launch_bounds__(256) void delta_grads(DeltaArgs a)
+template <typename D, bool BF, int DKP, bool VEC>
+__global__ __launch_bounds__(512) void delta_grads(DeltaArgs a)
 {
     using T = typename D::T;
     using M = Mat<BF>;
     using El = typename M::El;
     using Frag = typename M::Frag;
-    using Lds = GradsLds<D, BF, DKP>;
-    constexpr int TK = DKP / 16, KU = M::KU, TU = M::TU, UL = L / KU, VB = Lds::VB;
+    using Lds = GradsLds<BF, DKP>;
+    constexpr int TH = DKP / 32, KU = M::KU, UK = DKP / KU, UL = L / KU, VB = Lds::VB;
     __shared__ Lds s;
-    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, col = lane & 15, g4 = 4 * (lane >> 4);
+    const int tid = threadIdx.x, wave8 = tid >> 6, lane = tid & 63, col = lane & 15, g4 = 4 * (lane >> 4);
+    const int wave = wave8 & 3, half = wave8 >> 2, d0 = half * (DKP / 2);
     const int c = blockIdx.x % a.nc;
     const int64_t nh = blockIdx.x / a.nc;
     const int n = (int)(nh / a.Hk), hk = (int)(nh - (int64_t)n * a.Hk), group = a.Hv / a.Hk;
     const int t0 = c * L, live = max(0, min(L, length_of(a, n) - t0)), steps = min(L, a.T - t0);
     const int64_t row0 = (int64_t)t0 * a.N + n;
     const int i = 16 * wave + col;
-    f32x4 dq[TK], dk[TK];
+    f32x4 dq[TH], dk[TH];
 #pragma unroll
-    for (int t = 0; t < TK; ++t)
+    for (int t = 0; t < TH; ++t)
         dq[t] = dk[t] = f32x4{0, 0, 0, 0};
     if (live > 0) {
-        stage<D, El, DKP, 256>(s.k, Lds::LDK, (const T*)a.k + row0 * a.k_row + (int64_t)hk * a.Dk, (int64_t)a.N * a.k_row,
-                               live, a.Dk, a.vec_qk);
-        stage<D, El, DKP, 256>(s.q, Lds::LDK, (const T*)a.q + row0 * a.q_row + (int64_t)hk * a.Dk, (int64_t)a.N * a.q_row,
-                               live, a.Dk, a.vec_qk);
+        {
+            Rows<D, El, DKP, 512, VEC> k, q;
+            k.load((const T*)a.k + row0 * a.k_row + (int64_t)hk * a.Dk, a.k_step, live, a.Dk);
+            q.load((const T*)a.q + row0 * a.q_row + (int64_t)hk * a.Dk, a.q_step, live, a.Dk);
+            k.store(s.k, Lds::LDK, live, a.Dk);
+            q.store(s.q, Lds::LDK, live, a.Dk);
+        }
         __syncthreads();
-        f32x4 kk[4], kq[4];
+        // (K Q^T)[j][i] in the first half's waves, (K K^T)[j][i] in the second's
+        f32x4 kx[4];
 #pragma unroll
         for (int t = 0; t < 4; ++t)
-            kk[t] = kq[t] = f32x4{0, 0, 0, 0};
+            kx[t] = f32x4{0, 0, 0, 0};
+        const El* other = half ? s.k : s.q;
 #pragma unroll
-        for (int u = 0; u < DKP / KU; ++u) {
-            const Frag bk = M::rows(s.k + 16 * wave * Lds::LDK, Lds::LDK, u);
-            const Frag bq = M::rows(s.q + 16 * wave * Lds::LDK, Lds::LDK, u);
+        for (int u = 0; u < UK; ++u) {
+            const Frag b = M::rows(other + 16 * wave * Lds::LDK, Lds::LDK, u);
 #pragma unroll
             for (int t = 0; t < 4; ++t)
-                if (t <= wave) {
-                    const Frag ak = M::rows(s.k + 16 * t * Lds::LDK, Lds::LDK, u);
-                    kk[t] = M::mma(ak, bk, kk[t]);
-                    kq[t] = M::mma(ak, bq, kq[t]);
-                }
+                if (t <= wave)
+                    kx[t] = M::mma(M::rows(s.k + 16 * t * Lds::LDK, Lds::LDK, u), b, kx[t]);
         }
         for (int h = 0; h < group; ++h) {
             const int hv = hk * group + h;
             const int64_t unit = unit_of(a, n, hv, c);
-            if (wave == 0) {
-                const int64_t at = (row0 + (int64_t)lane * a.N) * a.Hv + hv;
-                const double G = running_sum(lane < live ? decay_of(D::get(((const T*)a.g)[at])) : 0.0);
+            Rows<D, El, VB, 512, VEC> no, nd;
+            Dense<El, VB, L, 512> nr;
+            Dense<El, VB, DKP, 512> n0, n1;
+            const auto fetch = [&](int v0) {
+                const int rows = min(VB, a.dvp - v0), cols = min(VB, a.Dv - v0);
+                const int64_t at = (row0 * a.Hv + hv) * a.Dv + v0;
+                no.load((const T*)a.grad_o + at, a.o_step, live, cols);
+                nd.load((const T*)a.grad_v + at, a.o_step, live, cols);
+                nr.load((const El*)a.U + (unit * a.dvp + v0) * L, rows);
+                n0.load((const El*)a.S0 + (unit * a.dvp + v0) * DKP, rows);
+                n1.load((const El*)a.dS + (unit * a.dvp + v0) * DKP, rows);
+            };
+            fetch(0);
+            if (wave8 == 0) {
+                const int64_t at = (row0 + (int64_t)min(lane, live - 1) * a.N) * a.Hv + hv;
+                const float gv = D::get(((const T*)a.g)[at]), bv = D::get(((const T*)a.beta)[at]);
+                const double G = running_sum(lane < live ? decay_of(gv) : 0.0);
                 s.G[lane] = G;
-                s.beta[lane] = lane < live ? D::get(((const T*)a.beta)[at]) : 0.0f;
+                s.beta[lane] = lane < live ? bv : 0.0f;
                 s.eG[lane] = expf((float)G);
                 s.to_end[lane] = expf((float)(__shfl(G, 63) - G));
             }
-            // products over the values
-            f32x4 qs[TK], ks[TK], ws[TK], dP[4], dA[4];
+            // products over the values: with the states (the half's keys), and r dO^T or r dV^T
+            f32x4 qs[TH], ks[TH], ws[TH], dX[4];
 #pragma unroll
-            for (int t = 0; t < TK; ++t)
+            for (int t = 0; t < TH; ++t)
                 qs[t] = ks[t] = ws[t] = f32x4{0, 0, 0, 0};
 #pragma unroll
             for (int t = 0; t < 4; ++t)
-                dP[t] = dA[t] = f32x4{0, 0, 0, 0};
+                dX[t] = f32x4{0, 0, 0, 0};
             float z = 0.0f;  // <S0, dS1>
             for (int v0 = 0; v0 < a.dvp; v0 += VB) {
                 const int rows = min(VB, a.dvp - v0), cols = min(VB, a.Dv - v0);
                 __syncthreads();
-                const int64_t at = (row0 * a.Hv + hv) * a.Dv + v0;
-                stage<D, El, VB, 256>(s.v.dO, Lds::LDV, (const T*)a.grad_o + at, (int64_t)a.N * a.Hv * a.Dv, live, cols,
-                                      a.vec_v);
-                stage<D, El, VB, 256>(s.v.dV, Lds::LDV, (const T*)a.grad_v + at, (int64_t)a.N * a.Hv * a.Dv, live, cols,
-                                      a.vec_v);
-                stage_dense<El, VB, L, 256>(s.v.r, Lds::LDL, (const El*)a.U + (unit * a.dvp + v0) * L, rows);
-                stage_dense<El, VB, DKP, 256>(s.v.S0, Lds::LDK, (const El*)a.S0 + (unit * a.dvp + v0) * DKP, rows);
-                stage_dense<El, VB, DKP, 256>(s.v.dS, Lds::LDK, (const El*)a.dS + (unit * a.dvp + v0) * DKP, rows);
+                no.store(s.v.dO, Lds::LDV, live, cols);
+                nd.store(s.v.dV, Lds::LDV, live, cols);
+                nr.store(s.v.r, Lds::LDL, rows);
+                n0.store(s.v.S0, Lds::LDK, rows);
+                n1.store(s.v.dS, Lds::LDK, rows);
                 __syncthreads();
-                for (int e = tid; e < VB * DKP; e += 256) {
-                    const int at2 = (e / DKP) * Lds::LDK + e % DKP;
-                    z = __builtin_fmaf(M::get(s.v.S0[at2]), M::get(s.v.dS[at2]), z);
-                }
+                if (v0 + VB < a.dvp)
+                    fetch(v0 + VB);
 #pragma unroll
                 for (int u = 0; u < VB / KU; ++u) {
                     const Frag bo = M::rows(s.v.dO + 16 * wave * Lds::LDV, Lds::LDV, u);
                     const Frag bv = M::rows(s.v.dV + 16 * wave * Lds::LDV, Lds::LDV, u);
                     const Frag br = M::cols(s.v.r + 16 * wave, Lds::LDL, u);
+                    Frag ar[4], as[TH];
+#pragma unroll
+                    for (int t = 0; t < TH; ++t)
+                        as[t] = M::cols(s.v.S0 + d0 + 16 * t, Lds::LDK, u);
 #pragma unroll
                     for (int t = 0; t < 4; ++t)
-                        if (t <= wave) {
-                            const Frag ar = M::cols(s.v.r + 16 * t, Lds::LDL, u);
-                            dP[t] = M::mma(ar, bo, dP[t]);
-                            dA[t] = M::mma(ar, bv, dA[t]);
-                        }
+                        ar[t] = M::cols(s.v.r + 16 * t, Lds::LDL, u);
+                    in_order();
 #pragma unroll
-                    for (int t = 0; t < TK; ++t) {
-                        const Frag as = M::cols(s.v.S0 + 16 * t, Lds::LDK, u);
-                        qs[t] = M::mma(as, bo, qs[t]);
-                        ks[t] = M::mma(as, bv, ks[t]);
-                        ws[t] = M::mma(M::cols(s.v.dS + 16 * t, Lds::LDK, u), br, ws[t]);
+                    for (int t = 0; t < TH; ++t) {
+                        qs[t] = M::mma(as[t], bo, qs[t]);
+                        ks[t] = M::mma(as[t], bv, ks[t]);
                     }
+                    in_order();
+#pragma unroll
+                    for (int t = 0; t < TH; ++t)
+                        as[t] = M::cols(s.v.dS + d0 + 16 * t, Lds::LDK, u);
+                    in_order();
+                    const Frag bx = half ? bv : bo;
+#pragma unroll
+                    for (int t = 0; t < 4; ++t)
+                        if (t <= wave)
+                            dX[t] = M::mma(ar[t], bx, dX[t]);
+#pragma unroll
+                    for (int t = 0; t < TH; ++t)
+                        ws[t] = M::mma(as[t], br, ws[t]);
+                    in_order();
+                }
+#pragma unroll
+                for (int e = tid * 4; e < VB * DKP; e += 2048) {
+                    const El* p0 = s.v.S0 + (e / DKP) * Lds::LDK + e % DKP;
+                    const El* p1 = s.v.dS + (e / DKP) * Lds::LDK + e % DKP;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        z = __builtin_fmaf(M::get(p0[j]), M::get(p1[j]), z);
                 }
             }
             __syncthreads();
-            // E^T, F^T in place of dP, dA; sums over i and j of their products with q.k and k.k
+            // E^T (first half) or F^T in place of the products; sums over i and over j of E q.k, F k.k
             const double Gi = s.G[i];
-            float row = 0.0f;
+            float row = 0.0f, diag = 0.0f;
 #pragma unroll
             for (int t = 0; t < 4; ++t) {
-                f32x4 y = {0, 0, 0, 0};
+                f32x4 y = {0, 0, 0, 0}, w = {0, 0, 0, 0};
+                if (t <= wave) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int j = 16 * t + g4 + e;
-                    const float m = t <= wave && j <= i ? expf((float)(Gi - s.G[j])) : 0.0f;
-                    const float E = a.scale * m * dP[t][e], F = j < i ? -m * dA[t][e] : 0.0f;
-                    y[e] = E * kq[t][e] + F * kk[t][e];
-                    const float b = s.beta[j];
-                    row = __builtin_fmaf(b, y[e], row);
-                    dP[t][e] = E * b;
-                    dA[t][e] = F * b;
+                    for (int e = 0; e < 4; ++e) {
+                        const int j = 16 * t + g4 + e;
+                        const float m = j <= i - half ? expf((float)(Gi - s.G[j])) : 0.0f;
+                        const float f = (half ? -m : a.scale * m) * dX[t][e], b = s.beta[j], both = f * kx[t][e];
+                        y[e] = j < i ? both : 0.0f;
+                        diag += j == i ? both : 0.0f;  // (one lane of the four that have step i)
+                        row = __builtin_fmaf(b, y[e], row);
+                        w[e] = f * b;
+                    }
+#pragma unroll
+                    for (int o = 1; o < 16; o <<= 1)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            y[e] += __shfl_xor(y[e], o);
                 }
-#pragma unroll
-                for (int o = 1; o < 16; o <<= 1)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        y[e] += __shfl_xor(y[e], o);
                 if (col == 0)
-                    *(f32x4*)(s.sum[wave] + 16 * t + g4) = y;
-                El* pe = s.m.E + i * Lds::LDL + 16 * t + g4;
-                El* pf = s.m.F + i * Lds::LDL + 16 * t + g4;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    pe[e] = M::put(dP[t][e]);
-                    pf[e] = M::put(dA[t][e]);
-                }
+                    *(f32x4*)(s.sum[wave8] + 16 * t + g4) = y;
+                put4<BF>(s.EF[half] + i * Lds::LDL + 16 * t + g4, w);
             }
-            row += __shfl_xor(row, 16);
-            row += __shfl_xor(row, 32);
             // products with the states, and what the gates take of them
             float ra = 0.0f, rx = 0.0f;
             const float eG = s.eG[i], to_end = s.to_end[i], bi = s.beta[i];
 #pragma unroll
-            for (int t = 0; t < TK; ++t)
+            for (int t = 0; t < TH; ++t) {
+                const El* pk = s.k + i * Lds::LDK + d0 + 16 * t + g4;
+                const El* pq = s.q + i * Lds::LDK + d0 + 16 * t + g4;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    const int d = 16 * t + g4 + e;
-                    const float kd = M::get(s.k[i * Lds::LDK + d]), qd = M::get(s.q[i * Lds::LDK + d]);
+                    const float kd = M::get(pk[e]), qd = M::get(pq[e]);
                     const float dq1 = a.scale * eG * qs[t][e], dk1 = eG * ks[t][e], dk2 = to_end * ws[t][e];
                     ra += qd * dq1 - kd * dk1;
                     rx += kd * dk2;
                     dq[t][e] += dq1;
                     dk[t][e] += bi * dk2 - dk1;
                 }
-            ra += __shfl_xor(ra, 16);
-            ra += __shfl_xor(ra, 32);
-            rx += __shfl_xor(rx, 16);
-            rx += __shfl_xor(rx, 32);
+            }
+#pragma unroll
+            for (int o = 16; o < 64; o <<= 1) {
+                row += __shfl_xor(row, o);
+                diag += __shfl_xor(diag, o);
+                ra += __shfl_xor(ra, o);
+                rx += __shfl_xor(rx, o);
+            }
             if (lane < 16) {
-                s.row[i] = row;
-                s.a[i] = ra;
-                s.x[i] = rx;
+                s.row[half][i] = row;
+                s.a[half][i] = ra;
+                s.x[half][i] = rx;
+                if (half == 0)
+                    s.diag[i] = diag;
             }
 #pragma unroll
             for (int o = 1; o < 64; o <<= 1)
                 z += __shfl_xor(z, o);
             if (lane == 0)
-                s.z[wave] = z;
+                s.z[wave8] = z;
             __syncthreads();
 #pragma unroll
             for (int u = 0; u < UL; ++u) {
-                const Frag bE = M::pack(dP + u * TU), bF = M::pack(dA + u * TU);
-                const Frag cE = M::cols(s.m.E + 16 * wave, Lds::LDL, u), cF = M::cols(s.m.F + 16 * wave, Lds::LDL, u);
+                const Frag bE = M::rows(s.EF[0] + 16 * wave * Lds::LDL, Lds::LDL, u);
+                const Frag bF = M::rows(s.EF[1] + 16 * wave * Lds::LDL, Lds::LDL, u);
+                const Frag cE = M::cols(s.EF[0] + 16 * wave, Lds::LDL, u), cF = M::cols(s.EF[1] + 16 * wave, Lds::LDL, u);
+                Frag ak[TH], aq[TH];
 #pragma unroll
-                for (int t = 0; t < TK; ++t) {
-                    const Frag ak = M::cols(s.k + 16 * t, Lds::LDK, u);
-                    dq[t] = M::mma(ak, bE, dq[t]);
-                    dk[t] = M::mma(ak, bF, dk[t]);
-                    dk[t] = M::mma(ak, cF, dk[t]);
-                    dk[t] = M::mma(M::cols(s.q + 16 * t, Lds::LDK, u), cE, dk[t]);
+                for (int t = 0; t < TH; ++t) {
+                    ak[t] = M::cols(s.k + d0 + 16 * t, Lds::LDK, u);
+                    aq[t] = M::cols(s.q + d0 + 16 * t, Lds::LDK, u);
                 }
+                in_order();
+#pragma unroll
+                for (int t = 0; t < TH; ++t) {
+                    dq[t] = M::mma(ak[t], bE, dq[t]);
+                    dk[t] = M::mma(ak[t], bF, dk[t]);
+                    dk[t] = M::mma(aq[t], cE, dk[t]);
+                    dk[t] = M::mma(ak[t], cF, dk[t]);
+                }
+                in_order();
             }
-            if (wave == 0) {
-                const float colsum = (s.sum[0][lane] + s.sum[1][lane]) + (s.sum[2][lane] + s.sum[3][lane]);
-                const float x = s.x[lane], b = s.beta[lane];
-                // sum_{i >= t} of what step i reads, less what it wrote: pairs with both ends behind t cancel
-                const double read = (double)s.a[lane] + s.row[lane] - (double)b * colsum, wrote = (double)b * x;
+            if (wave8 == 0) {
+                float colsum = 0.0f, zs = 0.0f;
+#pragma unroll
+                for (int w = 0; w < 8; ++w) {
+                    colsum += s.sum[w][lane];
+                    zs += s.z[w];
+                }
+                const float x = s.x[0][lane] + s.x[1][lane], b = s.beta[lane];
+                // sum_{i >= t} of what step i reads, less what it wrote: pairs with both ends behind t cancel (a
+                // step's own pair is left out of both, so a lone step's gradient is 0)
+                const double read = (double)s.a[0][lane] + s.a[1][lane] + s.row[0][lane] + s.row[1][lane] - (double)b * colsum;
+                const double wrote = (double)b * x;
                 const double upto = running_sum(read), before = running_sum(wrote) - wrote;
-                const double zz = (double)s.eG[L - 1] * (((double)s.z[0] + s.z[1]) + ((double)s.z[2] + s.z[3]));
-                const float dg = (float)(__shfl(upto, 63) - upto + read + before + zz);
-                const float db = colsum + x;
+                const float dg = (float)(__shfl(upto, 63) - upto + read + before + (double)s.eG[L - 1] * zs);
+                const float db = colsum + s.diag[lane] + x;
                 if (lane < steps) {
                     const int64_t at = (row0 + (int64_t)lane * a.N) * a.Hv + hv;
                     ((T*)a.grad_g)[at] = D::put(lane < live ? dg : 0.0f);
@@ -818,62 +1004,79 @@ __global__ __launch_bounds__(256) void delta_grads(DeltaArgs a)
     }
     if (i < steps) {
         const int64_t at = ((row0 + (int64_t)i * a.N) * a.Hk + hk) * a.Dk;
-        const float keep = i < live ? 1.0f : 0.0f;
+        T* pq = (T*)a.grad_q + at;
+        T* pk = (T*)a.grad_k + at;
 #pragma unroll
-        for (int t = 0; t < TK; ++t)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int d = 16 * t + g4 + e;
+        for (int t = 0; t < TH; ++t) {
+            const int d = d0 + 16 * t + g4;
+            if (i >= live)
+                dq[t] = dk[t] = f32x4{0, 0, 0, 0};
+            if (VEC) {  // (Dk is a multiple of 4 and the rows are aligned to them)
                 if (d < a.Dk) {
-                    ((T*)a.grad_q)[at + d] = D::put(keep * dq[t][e]);
-                    ((T*)a.grad_k)[at + d] = D::put(keep * dk[t][e]);
+                    put4<BF>((El*)pq + d, dq[t]);
+                    put4<BF>((El*)pk + d, dk[t]);
                 }
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (d + e < a.Dk) {
+                        pq[d + e] = D::put(dq[t][e]);
+                        pk[d + e] = D::put(dk[t][e]);
+                    }
             }
+        }
     }
 }
 
-template <typename D, bool BF, int DKP> hipError_t forward(const DeltaArgs& a, hipStream_t s)
+constexpr int kScanWaves = 4;
+
+int64_t scan_blocks(const DeltaArgs& a) { return (int64_t)a.N * a.Hv * ((a.dvp + 16 * kScanWaves - 1) / (16 * kScanWaves)); }
+
+template <typename D, bool BF, int DKP, bool VEC> hipError_t forward(const DeltaArgs& a, hipStream_t s)
 {
     if (a.nc > 0) {
-        delta_prep<D, BF, DKP><<<dim3((unsigned)((int64_t)a.N * a.Hk * a.nc)), dim3(256), 0, s>>>(a);
+        delta_prep<D, BF, DKP, VEC><<<dim3((unsigned)((int64_t)a.N * a.Hk * a.nc)), dim3(256), 0, s>>>(a);
         const hipError_t err = hipGetLastError();
         if (err != hipSuccess)
             return err;
     }
-    constexpr int NW = 4;
-    const int64_t blocks = (int64_t)a.N * a.Hv * ((a.dvp + 16 * NW - 1) / (16 * NW));
-    delta_scan<D, BF, DKP, NW><<<dim3((unsigned)blocks), dim3(NW * 64), 0, s>>>(a);
+    delta_scan<D, BF, DKP, kScanWaves, VEC><<<dim3((unsigned)scan_blocks(a)), dim3(kScanWaves * 64), 0, s>>>(a);
     return hipGetLastError();
 }
 
-template <typename D, bool BF, int DKP> hipError_t backward(const DeltaArgs& a, hipStream_t s)
+template <typename D, bool BF, int DKP, bool VEC> hipError_t backward(const DeltaArgs& a, hipStream_t s)
 {
-    constexpr int NW = 4;
-    const int64_t blocks = (int64_t)a.N * a.Hv * ((a.dvp + 16 * NW - 1) / (16 * NW));
-    delta_rscan<D, BF, DKP, NW><<<dim3((unsigned)blocks), dim3(NW * 64), 0, s>>>(a);
+    delta_rscan<D, BF, DKP, kScanWaves, VEC><<<dim3((unsigned)scan_blocks(a)), dim3(kScanWaves * 64), 0, s>>>(a);
     const hipError_t err = hipGetLastError();
     if (err != hipSuccess || a.nc == 0)
         return err;
-    delta_grads<D, BF, DKP><<<dim3((unsigned)((int64_t)a.N * a.Hk * a.nc)), dim3(256), 0, s>>>(a);
+    delta_grads<D, BF, DKP, VEC><<<dim3((unsigned)((int64_t)a.N * a.Hk * a.nc)), dim3(512), 0, s>>>(a);
     return hipGetLastError();
+}
+
+template <bool VEC> hipError_t run(const DeltaArgs& a, int dtype, bool bwd, hipStream_t s)
+{
+    const bool wide = delta_dkp(a.Dk) == 128;
+    if (dtype == kBF16) {
+        if (wide)
+            return bwd ? backward<StoreBF16, true, 128, VEC>(a, s) : forward<StoreBF16, true, 128, VEC>(a, s);
+        return bwd ? backward<StoreBF16, true, 64, VEC>(a, s) : forward<StoreBF16, true, 64, VEC>(a, s);
+    }
+    if (wide)
+        return bwd ? backward<StoreF32, false, 128, VEC>(a, s) : forward<StoreF32, false, 128, VEC>(a, s);
+    return bwd ? backward<StoreF32, false, 64, VEC>(a, s) : forward<StoreF32, false, 64, VEC>(a, s);
 }
 
 }  // namespace
 
 hipError_t launch_delta_forward(const DeltaArgs& a, int dtype, hipStream_t s)
 {
-    const bool wide = delta_dkp(a.Dk) == 128;
-    if (dtype == kBF16)
-        return wide ? forward<StoreBF16, kDeltaBf16Products, 128>(a, s) : forward<StoreBF16, kDeltaBf16Products, 64>(a, s);
-    return wide ? forward<StoreF32, false, 128>(a, s) : forward<StoreF32, false, 64>(a, s);
+    return a.vec_qk ? run<true>(a, dtype, false, s) : run<false>(a, dtype, false, s);
 }
 
 hipError_t launch_delta_backward(const DeltaArgs& a, int dtype, hipStream_t s)
 {
-    const bool wide = delta_dkp(a.Dk) == 128;
-    if (dtype == kBF16)
-        return wide ? backward<StoreBF16, kDeltaBf16Products, 128>(a, s) : backward<StoreBF16, kDeltaBf16Products, 64>(a, s);
-    return wide ? backward<StoreF32, false, 128>(a, s) : backward<StoreF32, false, 64>(a, s);
+    return a.vec_qk && a.vec_v ? run<true>(a, dtype, true, s) : run<false>(a, dtype, true, s);
 }
 
 }  // namespace mfpsn

@@ -116,57 +116,106 @@ struct StoreBF16 {
     __device__ static T put(float v) { return (__bf16)v; }  // to nearest even
 };
 
-// 64 rows of `cols` elements from memory (`stride` elements apart; rows from
-// `live` on are not read) into LDS rows of `ld` elements, zeros behind `live` and
-// from `cols` up to COLS.  vec: rows are 16-byte aligned and cols a multiple of 16 bytes.
-template <typename D, typename El, int COLS, int THREADS, int ROWS = 64>
-__device__ __forceinline__ void stage(El* lds, int ld, const typename D::T* src, int64_t stride, int live, int cols,
-                                      bool vec)
+// Keeps what stands before it before what stands behind it.  The operands of
+// several products are read from LDS together, one group ahead of the products
+// that use them; left to itself the compiler reads each where it is used and
+// waits for it, about 100 cycles a product.
+__device__ __forceinline__ void in_order() { __builtin_amdgcn_sched_barrier(0); }
+
+// Address of row r, rows `stride` bytes apart
+template <typename T> __device__ __forceinline__ const T* row_at(const T* p, int r, uint32_t stride)
 {
-    using T = typename D::T;
-    constexpr int VE = 16 / sizeof(T), PER = COLS / VE;
-    static_assert(COLS % VE == 0);
-    for (int i = threadIdx.x; i < ROWS * PER; i += THREADS) {
-        const int r = i / PER, c = (i - r * PER) * VE;
-        alignas(16) T e[VE];
-#pragma unroll
-        for (int j = 0; j < VE; ++j)
-            e[j] = D::put(0.0f);
-        if (r < live && c < cols) {
-            const T* s = src + (int64_t)r * stride + c;
-            if (vec) {
-                *(uint4*)e = *(const uint4*)s;
-            } else {
-#pragma unroll
-                for (int j = 0; j < VE; ++j)
-                    if (c + j < cols)
-                        e[j] = s[j];
-            }
-        }
-        El* d = lds + r * ld + c;
-        if constexpr (sizeof(El) == sizeof(T)) {
-            *(uint4*)d = *(const uint4*)e;
-        } else {
-#pragma unroll
-            for (int j = 0; j < VE; ++j)
-                d[j] = (El)D::get(e[j]);
-        }
-    }
+    return (const T*)((const char*)p + (uint64_t)(uint32_t)r * stride);
 }
 
-// ROWS x COLS elements lying densely in memory into LDS rows of `ld` elements;
-// rows from `live` on become zeros
-template <typename El, int ROWS, int COLS, int THREADS>
-__device__ __forceinline__ void stage_dense(El* lds, int ld, const El* src, int live = ROWS)
-{
-    constexpr int VE = 16 / sizeof(El), PER = COLS / VE;
-    for (int i = threadIdx.x; i < ROWS * PER; i += THREADS) {
-        const int r = i / PER, c = (i - r * PER) * VE;
-        uint4 v = {0, 0, 0, 0};
-        if (r < live)
-            v = *(const uint4*)(src + (int64_t)r * COLS + c);
-        *(uint4*)(lds + r * ld + c) = v;
+// ROWS rows of `cols` elements from memory, `stride` bytes apart, on their way
+// into LDS rows of `ld` elements: load() issues every read at once (the values
+// wait in registers, so that reads of the next tile run while this one is
+// computed with), store() writes them, zeros in rows from `live` on and from
+// column `cols` to COLS.  Reads outside that range go to the last row or first
+// column instead (live >= 1), never outside the tensor.  VEC: rows are 16-byte
+// aligned and cols is a multiple of 16 bytes.
+template <typename D, typename El, int COLS, int THREADS, bool VEC, int ROWS = 64> struct Rows {
+    using T = typename D::T;
+    static constexpr int VE = 16 / sizeof(T), PER = COLS / VE, STEP = THREADS / PER, NL = (ROWS + STEP - 1) / STEP;
+    static_assert(COLS % VE == 0 && THREADS % PER == 0);
+    uint4 v[NL];
+
+    __device__ __forceinline__ void load(const T* src, uint32_t stride, int live, int cols)
+    {
+        const int r0 = threadIdx.x / PER, c = (threadIdx.x % PER) * VE;
+        if constexpr (VEC) {
+            const T* p = src + (c < cols ? c : 0);
+#pragma unroll
+            for (int n = 0; n < NL; ++n)
+                v[n] = *(const uint4*)row_at(p, min(r0 + n * STEP, live - 1), stride);
+        } else {
+#pragma unroll
+            for (int n = 0; n < NL; ++n) {
+                const T* p = row_at(src, min(r0 + n * STEP, live - 1), stride);
+                alignas(16) T e[VE];
+#pragma unroll
+                for (int j = 0; j < VE; ++j) {
+                    e[j] = p[c + j < cols ? c + j : 0];
+                    if (c + j >= cols)
+                        e[j] = D::put(0.0f);
+                }
+                v[n] = *(const uint4*)e;
+            }
+        }
     }
+    __device__ __forceinline__ void store(El* lds, int ld, int live, int cols)
+    {
+        const int r0 = threadIdx.x / PER, c = (threadIdx.x % PER) * VE;
+#pragma unroll
+        for (int n = 0; n < NL; ++n) {
+            const int r = r0 + n * STEP;
+            if (ROWS % STEP != 0 && r >= ROWS)
+                break;
+            const bool in = r < live && c < cols;
+            const uint4 w = {in ? v[n].x : 0, in ? v[n].y : 0, in ? v[n].z : 0, in ? v[n].w : 0};
+            El* d = lds + r * ld + c;
+            static_assert(sizeof(El) == sizeof(T));
+            *(uint4*)d = w;
+        }
+    }
+};
+
+// The same for ROWS x COLS elements that lie densely in one of the kernels' own
+// arrays; rows from `live` (>= 1) on become zeros
+template <typename El, int ROWS, int COLS, int THREADS> struct Dense {
+    static constexpr int VE = 16 / sizeof(El), PER = COLS / VE, STEP = THREADS / PER, NL = (ROWS + STEP - 1) / STEP;
+    static_assert(THREADS % PER == 0);
+    uint4 v[NL];
+
+    __device__ __forceinline__ void load(const El* src, int live = ROWS)
+    {
+        const int r0 = threadIdx.x / PER, c = (threadIdx.x % PER) * VE;
+#pragma unroll
+        for (int n = 0; n < NL; ++n)
+            v[n] = *(const uint4*)(src + min(r0 + n * STEP, live - 1) * COLS + c);
+    }
+    __device__ __forceinline__ void store(El* lds, int ld, int live = ROWS)
+    {
+        const int r0 = threadIdx.x / PER, c = (threadIdx.x % PER) * VE;
+#pragma unroll
+        for (int n = 0; n < NL; ++n) {
+            const int r = r0 + n * STEP;
+            if (ROWS % STEP != 0 && r >= ROWS)
+                break;
+            const bool in = r < live;
+            *(uint4*)(lds + r * ld + c) = uint4{in ? v[n].x : 0, in ? v[n].y : 0, in ? v[n].z : 0, in ? v[n].w : 0};
+        }
+    }
+};
+
+// Four consecutive values of a result tile's column
+template <bool BF> __device__ __forceinline__ void put4(typename Mat<BF>::El* p, const f32x4 v)
+{
+    if constexpr (BF)
+        *(bf16x4*)p = bf16x4{(__bf16)v[0], (__bf16)v[1], (__bf16)v[2], (__bf16)v[3]};
+    else
+        *(f32x4*)p = v;
 }
 
 }  // namespace mfpsn
