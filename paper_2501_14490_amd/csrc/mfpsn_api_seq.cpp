@@ -92,6 +92,10 @@ void fill(DeltaArgs& a, const mfpsn_delta_desc* d, const void* q, const void* k,
     a.v_step = (uint32_t)(a.v_row * a.N * es);
     a.o_step = (uint32_t)((int64_t)a.N * a.Hv * a.Dv * es);
     a.g_step = (uint32_t)((int64_t)a.N * a.Hv * es);
+    uint32_t longest = a.o_step > a.v_step ? a.o_step : a.v_step;
+    longest = a.q_step > longest ? a.q_step : longest;
+    longest = a.k_step > longest ? a.k_step : longest;
+    a.near = longest <= UINT32_MAX / 64;
     a.vec_qk = wide_rows(q, a.q_row, d->Dk, es) && wide_rows(k, a.k_row, d->Dk, es);
     a.nc = (int32_t)(((int64_t)d->T + kDeltaChunk - 1) / kDeltaChunk);
     a.dvp = (d->Dv + 15) / 16 * 16;

@@ -20,6 +20,7 @@ struct DeltaArgs {
     float scale;
     int64_t q_row, k_row, v_row;  // elements between the rows of consecutive (t, n)
     uint32_t q_step, k_step, v_step, o_step, g_step;  // bytes between consecutive t (o: grad_o and grad_v too)
+    int32_t near;                 // 64 of the longest of these steps fit 32 bits
     int32_t vec_qk, vec_v;        // rows of q and k (of the gradients) may be read and written 16 bytes at a time
     int32_t nc;                   // chunks of the longest sequence
     int32_t dvp;                  // Dv rounded up to 16
@@ -30,7 +31,7 @@ struct DeltaArgs {
     float* state_out;             // nullable
     // per (sequence, value head, chunk), see delta_layout
     void *X, *P, *S0, *U;         // S0, U: nullable in the forward (not saved)
-    float* gate;                  // [2][64]: e^G, e^(G_last - G)
+    float* gate;                  // [3][64]: e^G, scale e^G, e^(G_last - G) beta
     // backward
     const void* grad_o;
     const float* grad_state_out;  // nullable: zeros
@@ -62,7 +63,7 @@ inline DeltaLayout delta_layout(int64_t T, int64_t N, int64_t Hv, int Dk, int Dv
     l.units = (size_t)N * (size_t)Hv * (size_t)((T + kDeltaChunk - 1) / kDeltaChunk);
     l.x = L * L * 4;
     l.p = L * L * (size_t)es;
-    l.gate = 2 * L * 4;
+    l.gate = 3 * L * 4;
     l.u = dvp * L * (size_t)es;
     l.s0 = dvp * dkp * (size_t)es;
     return l;

@@ -164,8 +164,8 @@ __global__ __launch_bounds__(256) void delta_prep(DeltaArgs a)
     const int64_t row0 = (int64_t)t0 * a.N + n;
     {
         Rows<D, El, DKP, 256, VEC> k, q;
-        k.load((const T*)a.k + row0 * a.k_row + (int64_t)hk * a.Dk, a.k_step, live, a.Dk);
-        q.load((const T*)a.q + row0 * a.q_row + (int64_t)hk * a.Dk, a.q_step, live, a.Dk);
+        k.load((const T*)a.k + row0 * a.k_row + (int64_t)hk * a.Dk, a.k_step, live, a.Dk, a.near);
+        q.load((const T*)a.q + row0 * a.q_row + (int64_t)hk * a.Dk, a.q_step, live, a.Dk, a.near);
         k.store(s.k, Lds::LDK, live, a.Dk);
         q.store(s.q, Lds::LDK, live, a.Dk);
     }
@@ -195,11 +195,13 @@ __global__ __launch_bounds__(256) void delta_prep(DeltaArgs a)
         if (wave == 0) {
             const int64_t at = (row0 + (int64_t)lane * a.N) * a.Hv + hv;
             const double G = running_sum(lane < live ? decay_of(D::get(((const T*)a.g)[at])) : 0.0);
+            const float b = lane < live ? D::get(((const T*)a.beta)[at]) : 0.0f, eG = expf((float)G);
             s.G[lane] = G;
-            s.beta[lane] = lane < live ? D::get(((const T*)a.beta)[at]) : 0.0f;
-            float* gate = a.gate + unit * 2 * L;
-            gate[lane] = expf((float)G);
-            gate[L + lane] = expf((float)(__shfl(G, 63) - G));
+            s.beta[lane] = b;
+            float* gate = a.gate + unit * 3 * L;
+            gate[lane] = eG;
+            gate[L + lane] = a.scale * eG;
+            gate[2 * L + lane] = expf((float)(__shfl(G, 63) - G)) * b;
         }
         __syncthreads();
         El* P = (El*)a.P + unit * L * L;
@@ -257,7 +259,7 @@ template <bool BF, int DKP> struct ScanLds {
     static constexpr int LDK = DKP + Mat<BF>::PAD, LDL = L + Mat<BF>::PAD;
     El k[L * LDK], q[L * LDK];
     El x[BF ? 2 : 1][L * LDL], p[L * LDL];
-    float gate[2 * L], beta[L];
+    float gate[3 * L];
 };
 
 template <typename D, bool BF, int DKP, int NW, bool VEC>
@@ -269,7 +271,7 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(1, 1)))
     using Frag = typename M::Frag;
     using Lds = ScanLds<BF, DKP>;
     constexpr int TK = DKP / 16, TH = NW * 64, KU = M::KU, TU = M::TU, UK = DKP / KU, UL = L / KU;
-    static_assert(TH >= 2 * L);
+    static_assert(TH >= 3 * L);
     __shared__ Lds s;
     const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, col = lane & 15, g4 = 4 * (lane >> 4);
     const int vblocks = (a.dvp + 16 * NW - 1) / (16 * NW);
@@ -289,25 +291,19 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(1, 1)))
         }
     Rows<D, El, DKP, TH, VEC> nk, nq;
     Dense<El, L, L, TH> nx[BF ? 2 : 1], np;
-    T nv[16];
-    float ngate = 0.0f, nbeta = 0.0f;
+    Column<T> nv;
+    float ngate;
     const auto fetch = [&](int c) {
         const int t0 = c * L, live = min(L, len - t0);
         const int64_t row0 = (int64_t)t0 * a.N + n, unit = unit_of(a, n, hv, c);
-        nk.load((const T*)a.k + row0 * a.k_row + (int64_t)hk * a.Dk, a.k_step, live, a.Dk);
-        nq.load((const T*)a.q + row0 * a.q_row + (int64_t)hk * a.Dk, a.q_step, live, a.Dk);
+        nk.load((const T*)a.k + row0 * a.k_row + (int64_t)hk * a.Dk, a.k_step, live, a.Dk, a.near);
+        nq.load((const T*)a.q + row0 * a.q_row + (int64_t)hk * a.Dk, a.q_step, live, a.Dk, a.near);
         nx[0].load((const El*)a.X + unit * L * L * (BF ? 2 : 1));
         if constexpr (BF)
             nx[1].load((const El*)a.X + unit * L * L * 2 + L * L);
         np.load((const El*)a.P + unit * L * L);
-        const T* pv = (const T*)a.v + row0 * a.v_row + (int64_t)hv * a.Dv + (mine ? v : 0);
-#pragma unroll
-        for (int e = 0; e < 16; ++e)
-            nv[e] = *row_at(pv, min(16 * (e >> 2) + g4 + (e & 3), live - 1), a.v_step);
-        if (tid < 2 * L)
-            ngate = a.gate[unit * 2 * L + tid];
-        if (tid < L)
-            nbeta = D::get(*row_at((const T*)a.beta + row0 * a.Hv + hv, min(tid, live - 1), a.g_step));
+        nv.load((const T*)a.v + row0 * a.v_row + (int64_t)hv * a.Dv, mine ? v : 0, a.v_step, live, a.near);
+        ngate = a.gate[unit * 3 * L + min(tid, 3 * L - 1)];
     };
     if (chunks > 0)
         fetch(0);
@@ -321,16 +317,19 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(1, 1)))
         if constexpr (BF)
             nx[1].store(s.x[1], Lds::LDL);
         np.store(s.p, Lds::LDL);
-        if (tid < 2 * L)
+        if (tid < 3 * L)
             s.gate[tid] = ngate;
-        if (tid < L)
-            s.beta[tid] = tid < live ? nbeta : 0.0f;
         f32x4 R[4];
 #pragma unroll
         for (int t = 0; t < 4; ++t)
+            R[t] = f32x4{D::get(nv.x[t][0]), D::get(nv.x[t][1]), D::get(nv.x[t][2]), D::get(nv.x[t][3])};
+        if (live < L || !mine) {
 #pragma unroll
-            for (int r = 0; r < 4; ++r)
-                R[t][r] = mine && 16 * t + g4 + r < live ? D::get(nv[4 * t + r]) : 0.0f;
+            for (int t = 0; t < 4; ++t)
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    R[t][r] = mine && 16 * t + g4 + r < live ? R[t][r] : 0.0f;
+        }
         __syncthreads();
         if (c + 1 < chunks)
             fetch(c + 1);
@@ -341,7 +340,7 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(1, 1)))
                 put4<BF>(S0 + 16 * t + g4, S[t]);
         }
         // K S0 and Q S0.  16-bit: the state goes in as the sum of two numbers of 8 bits each.
-        f32x4 KS[4], O[4], eG[4], to_end[4];
+        f32x4 KS[4], O[4], eG[4], sG[4], gam[4];
         Frag fk[2][4], fq[2][4], fx[UL][4], fl[UL][4], fp[UL][4], ft[2][TK];
         const auto read_kq = [&](int u) {
 #pragma unroll
@@ -363,7 +362,8 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(1, 1)))
 #pragma unroll
                 for (int t = 0; t < 4; ++t) {
                     eG[t] = *(const f32x4*)(s.gate + 16 * t + g4);
-                    to_end[t] = *(const f32x4*)(s.gate + L + 16 * t + g4) * *(const f32x4*)(s.beta + 16 * t + g4);
+                    sG[t] = *(const f32x4*)(s.gate + L + 16 * t + g4);
+                    gam[t] = *(const f32x4*)(s.gate + 2 * L + 16 * t + g4);
                 }
 #pragma unroll
                 for (int w = 0; w < UL; ++w)
@@ -407,7 +407,7 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(1, 1)))
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 R[t][r] = __builtin_fmaf(-eG[t][r], KS[t][r], R[t][r]);
-                O[t][r] *= a.scale * eG[t][r];
+                O[t][r] *= sG[t][r];
             }
         }
 #pragma unroll
@@ -462,7 +462,7 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(1, 1)))
         for (int t = 0; t < 4; ++t)
 #pragma unroll
             for (int r = 0; r < 4; ++r)
-                U[t][r] *= to_end[t][r];
+                U[t][r] *= gam[t][r];
 #pragma unroll
         for (int t = 0; t < TK; ++t)
 #pragma unroll
@@ -485,15 +485,8 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(1, 1)))
             }
             in_order();
         }
-        T* po = (T*)a.o + (row0 * a.Hv + hv) * a.Dv + v;
-#pragma unroll
-        for (int t = 0; t < 4; ++t)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int i = 16 * t + g4 + r;
-                if (mine && i < live)
-                    *const_cast<T*>(row_at(po, i, a.o_step)) = D::put(O[t][r]);
-            }
+        if (mine)
+            store_column<D>(O, (T*)a.o + (row0 * a.Hv + hv) * a.Dv, v, a.o_step, live, a.near);
     }
     if (!mine)
         return;
@@ -516,7 +509,7 @@ template <bool BF, int DKP> struct RscanLds {
     using El = typename Mat<BF>::El;
     static constexpr int LDK = DKP + Mat<BF>::PAD, LDL = L + Mat<BF>::PAD;
     El k[L * LDK], q[L * LDK], x[L * LDL], p[L * LDL];
-    float gate[2 * L], beta[L];
+    float gate[3 * L];
 };
 
 template <typename D, bool BF, int DKP, int NW, bool VEC>
@@ -528,7 +521,7 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(1, 1)))
     using Frag = typename M::Frag;
     using Lds = RscanLds<BF, DKP>;
     constexpr int TK = DKP / 16, TH = NW * 64, KU = M::KU, TU = M::TU, UK = DKP / KU, UL = L / KU;
-    static_assert(TH >= 2 * L);
+    static_assert(TH >= 3 * L);
     __shared__ Lds s;
     const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, col = lane & 15, g4 = 4 * (lane >> 4);
     const int vblocks = (a.dvp + 16 * NW - 1) / (16 * NW);
@@ -547,23 +540,17 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(1, 1)))
         }
     Rows<D, El, DKP, TH, VEC> nk, nq;
     Dense<El, L, L, TH> nx, np;
-    T no[16];
-    float ngate = 0.0f, nbeta = 0.0f;
+    Column<T> no;
+    float ngate;
     const auto fetch = [&](int c) {
         const int t0 = c * L, live = min(L, len - t0);
         const int64_t row0 = (int64_t)t0 * a.N + n, unit = unit_of(a, n, hv, c);
-        nk.load((const T*)a.k + row0 * a.k_row + (int64_t)hk * a.Dk, a.k_step, live, a.Dk);
-        nq.load((const T*)a.q + row0 * a.q_row + (int64_t)hk * a.Dk, a.q_step, live, a.Dk);
+        nk.load((const T*)a.k + row0 * a.k_row + (int64_t)hk * a.Dk, a.k_step, live, a.Dk, a.near);
+        nq.load((const T*)a.q + row0 * a.q_row + (int64_t)hk * a.Dk, a.q_step, live, a.Dk, a.near);
         nx.load((const El*)a.X + unit * L * L * (BF ? 2 : 1));
         np.load((const El*)a.P + unit * L * L);
-        const T* po = (const T*)a.grad_o + (row0 * a.Hv + hv) * a.Dv + (mine ? v : 0);
-#pragma unroll
-        for (int e = 0; e < 16; ++e)
-            no[e] = *row_at(po, min(16 * (e >> 2) + g4 + (e & 3), live - 1), a.o_step);
-        if (tid < 2 * L)
-            ngate = a.gate[unit * 2 * L + tid];
-        if (tid < L)
-            nbeta = D::get(*row_at((const T*)a.beta + row0 * a.Hv + hv, min(tid, live - 1), a.g_step));
+        no.load((const T*)a.grad_o + (row0 * a.Hv + hv) * a.Dv, mine ? v : 0, a.o_step, live, a.near);
+        ngate = a.gate[unit * 3 * L + min(tid, 3 * L - 1)];
     };
     if (chunks > 0)
         fetch(chunks - 1);
@@ -575,16 +562,19 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(1, 1)))
         nq.store(s.q, Lds::LDK, live, a.Dk);
         nx.store(s.x, Lds::LDL);
         np.store(s.p, Lds::LDL);
-        if (tid < 2 * L)
+        if (tid < 3 * L)
             s.gate[tid] = ngate;
-        if (tid < L)
-            s.beta[tid] = tid < live ? nbeta : 0.0f;
         f32x4 dO[4];
 #pragma unroll
         for (int t = 0; t < 4; ++t)
+            dO[t] = f32x4{D::get(no.x[t][0]), D::get(no.x[t][1]), D::get(no.x[t][2]), D::get(no.x[t][3])};
+        if (live < L || !mine) {
 #pragma unroll
-            for (int r = 0; r < 4; ++r)
-                dO[t][r] = mine && 16 * t + g4 + r < live ? D::get(no[4 * t + r]) : 0.0f;
+            for (int t = 0; t < 4; ++t)
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    dO[t][r] = mine && 16 * t + g4 + r < live ? dO[t][r] : 0.0f;
+        }
         __syncthreads();
         if (c > 0)
             fetch(c - 1);
@@ -595,7 +585,7 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(1, 1)))
                 put4<BF>(dS + 16 * t + g4, S[t]);
         }
         // dr' = diag(e^{G_last - G} beta) K dS1 + P^T dO
-        f32x4 R[4], eG[4], to_end[4];
+        f32x4 R[4], eG[4], sG[4], gam[4];
         Frag fk[2][4], fp[UL][4], fx[UL][4], ft[2][TK];
         const auto read_k = [&](int u) {
 #pragma unroll
@@ -615,7 +605,8 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(1, 1)))
 #pragma unroll
                 for (int t = 0; t < 4; ++t) {
                     eG[t] = *(const f32x4*)(s.gate + 16 * t + g4);
-                    to_end[t] = *(const f32x4*)(s.gate + L + 16 * t + g4) * *(const f32x4*)(s.beta + 16 * t + g4);
+                    sG[t] = *(const f32x4*)(s.gate + L + 16 * t + g4);
+                    gam[t] = *(const f32x4*)(s.gate + 2 * L + 16 * t + g4);
                 }
 #pragma unroll
                 for (int w = 0; w < UL; ++w)
@@ -648,7 +639,7 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(1, 1)))
         for (int t = 0; t < 4; ++t)
 #pragma unroll
             for (int r = 0; r < 4; ++r)
-                R[t][r] *= to_end[t][r];
+                R[t][r] *= gam[t][r];
 #pragma unroll
         for (int u = 0; u < UL; ++u) {
             const Frag b = M::pack(dO + u * TU);
@@ -665,7 +656,7 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(1, 1)))
             dV[t] = f32x4{0, 0, 0, 0};
 #pragma unroll
             for (int r = 0; r < 4; ++r)
-                dO[t][r] *= a.scale * eG[t][r];
+                dO[t][r] *= sG[t][r];
         }
 #pragma unroll
         for (int t = 0; t < TK; ++t)
@@ -693,16 +684,13 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(1, 1)))
                 if ((u + 1) * KU > 16 * t)
                     dV[t] = M::mma(fx[u][t], b, dV[t]);
         }
-        T* pv = (T*)a.grad_v + (row0 * a.Hv + hv) * a.Dv + v;
+        if (mine)
+            store_column<D>(dV, (T*)a.grad_v + (row0 * a.Hv + hv) * a.Dv, v, a.o_step, live, a.near);
 #pragma unroll
         for (int t = 0; t < 4; ++t)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                const int i = 16 * t + g4 + r;
-                if (mine && i < live)
-                    *const_cast<T*>(row_at(pv, i, a.o_step)) = D::put(dV[t][r]);
+            for (int r = 0; r < 4; ++r)
                 dV[t][r] *= -eG[t][r];
-            }
 #pragma unroll
         for (int u = 0; u < UL; ++u) {
             if (u + 1 < UL)
@@ -777,28 +765,9 @@ __global__ __launch_bounds__(512) void delta_grads(DeltaArgs a)
     for (int t = 0; t < TH; ++t)
         dq[t] = dk[t] = f32x4{0, 0, 0, 0};
     if (live > 0) {
-        {
-            Rows<D, El, DKP, 512, VEC> k, q;
-            k.load((const T*)a.k + row0 * a.k_row + (int64_t)hk * a.Dk, a.k_step, live, a.Dk);
-            q.load((const T*)a.q + row0 * a.q_row + (int64_t)hk * a.Dk, a.q_step, live, a.Dk);
-            k.store(s.k, Lds::LDK, live, a.Dk);
-            q.store(s.q, Lds::LDK, live, a.Dk);
-        }
-        __syncthreads();
-        // (K Q^T)[j][i] in the first half's waves, (K K^T)[j][i] in the second's
-        f32x4 kx[4];
-#pragma unroll
-        for (int t = 0; t < 4; ++t)
-            kx[t] = f32x4{0, 0, 0, 0};
-        const El* other = half ? s.k : s.q;
-#pragma unroll
-        for (int u = 0; u < UK; ++u) {
-            const Frag b = M::rows(other + 16 * wave * Lds::LDK, Lds::LDK, u);
-#pragma unroll
-            for (int t = 0; t < 4; ++t)
-                if (t <= wave)
-                    kx[t] = M::mma(M::rows(s.k + 16 * t * Lds::LDK, Lds::LDK, u), b, kx[t]);
-        }
+        Rows<D, El, DKP, 512, VEC> nk, nq;
+        nk.load((const T*)a.k + row0 * a.k_row + (int64_t)hk * a.Dk, a.k_step, live, a.Dk, a.near);
+        nq.load((const T*)a.q + row0 * a.q_row + (int64_t)hk * a.Dk, a.q_step, live, a.Dk, a.near);
         for (int h = 0; h < group; ++h) {
             const int hv = hk * group + h;
             const int64_t unit = unit_of(a, n, hv, c);
@@ -808,8 +777,8 @@ __global__ __launch_bounds__(512) void delta_grads(DeltaArgs a)
             const auto fetch = [&](int v0) {
                 const int rows = min(VB, a.dvp - v0), cols = min(VB, a.Dv - v0);
                 const int64_t at = (row0 * a.Hv + hv) * a.Dv + v0;
-                no.load((const T*)a.grad_o + at, a.o_step, live, cols);
-                nd.load((const T*)a.grad_v + at, a.o_step, live, cols);
+                no.load((const T*)a.grad_o + at, a.o_step, live, cols, a.near);
+                nd.load((const T*)a.grad_v + at, a.o_step, live, cols, a.near);
                 nr.load((const El*)a.U + (unit * a.dvp + v0) * L, rows);
                 n0.load((const El*)a.S0 + (unit * a.dvp + v0) * DKP, rows);
                 n1.load((const El*)a.dS + (unit * a.dvp + v0) * DKP, rows);
@@ -836,6 +805,10 @@ __global__ __launch_bounds__(512) void delta_grads(DeltaArgs a)
             for (int v0 = 0; v0 < a.dvp; v0 += VB) {
                 const int rows = min(VB, a.dvp - v0), cols = min(VB, a.Dv - v0);
                 __syncthreads();
+                if (h == 0 && v0 == 0) {
+                    nk.store(s.k, Lds::LDK, live, a.Dk);
+                    nq.store(s.q, Lds::LDK, live, a.Dk);
+                }
                 no.store(s.v.dO, Lds::LDV, live, cols);
                 nd.store(s.v.dV, Lds::LDV, live, cols);
                 nr.store(s.v.r, Lds::LDL, rows);
@@ -887,6 +860,25 @@ __global__ __launch_bounds__(512) void delta_grads(DeltaArgs a)
                 }
             }
             __syncthreads();
+            // (K Q^T)[j][i] in the first half's waves, (K K^T)[j][i] in the second's
+            f32x4 kx[4];
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+                kx[t] = f32x4{0, 0, 0, 0};
+            const El* other = half ? s.k : s.q;
+#pragma unroll
+            for (int u = 0; u < UK; ++u) {
+                const Frag b = M::rows(other + 16 * wave * Lds::LDK, Lds::LDK, u);
+                Frag ak[4];
+#pragma unroll
+                for (int t = 0; t < 4; ++t)
+                    ak[t] = M::rows(s.k + 16 * t * Lds::LDK, Lds::LDK, u);
+                in_order();
+#pragma unroll
+                for (int t = 0; t < 4; ++t)
+                    if (t <= wave)
+                        kx[t] = M::mma(ak[t], b, kx[t]);
+            }
             // E^T (first half) or F^T in place of the products; sums over i and over j of E q.k, F k.k
             const double Gi = s.G[i];
             float row = 0.0f, diag = 0.0f;

@@ -23,6 +23,8 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef short i16x4 __attribute__((ext_vector_type(4)));
+typedef float f32x8 __attribute__((ext_vector_type(8)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 __device__ __forceinline__ f32x4 mfma_f32(const f32x4 a, const f32x4 b, f32x4 c)
 {
@@ -84,20 +86,17 @@ template <> struct Mat<true> {
     }
     __device__ static Frag pack(const f32x4* t)
     {
-        Frag f;
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-            f[i] = (__bf16)t[i >> 2][i & 3];
-        return f;
+        return __builtin_convertvector(__builtin_shufflevector(t[0], t[1], 0, 1, 2, 3, 4, 5, 6, 7), Frag);
     }
     // what pack() left of each value, as the next 8 bits
     __device__ static Frag pack_rest(const f32x4* t, Frag hi)
     {
-        Frag f;
+        const u32x4 h = __builtin_bit_cast(u32x4, hi);
+        f32x8 f;
 #pragma unroll
         for (int i = 0; i < 8; ++i)
-            f[i] = (__bf16)(t[i >> 2][i & 3] - (float)hi[i]);
-        return f;
+            f[i] = t[i >> 2][i & 3] - __builtin_bit_cast(float, i & 1 ? h[i >> 1] & 0xffff0000u : h[i >> 1] << 16);
+        return __builtin_convertvector(f, Frag);
     }
     __device__ static f32x4 mma(Frag a, Frag b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
     __device__ static El put(float v) { return (__bf16)v; }
@@ -134,21 +133,31 @@ template <typename T> __device__ __forceinline__ const T* row_at(const T* p, int
 // computed with), store() writes them, zeros in rows from `live` on and from
 // column `cols` to COLS.  Reads outside that range go to the last row or first
 // column instead (live >= 1), never outside the tensor.  VEC: rows are 16-byte
-// aligned and cols is a multiple of 16 bytes.
+// aligned and cols is a multiple of 16 bytes.  near: ROWS * stride fits 32 bits;
+// a whole tile is then read at one 32-bit offset a thread behind scalar row
+// addresses, which leaves no address arithmetic to the lanes.
 template <typename D, typename El, int COLS, int THREADS, bool VEC, int ROWS = 64> struct Rows {
     using T = typename D::T;
+    static_assert(sizeof(El) == sizeof(T));
     static constexpr int VE = 16 / sizeof(T), PER = COLS / VE, STEP = THREADS / PER, NL = (ROWS + STEP - 1) / STEP;
-    static_assert(COLS % VE == 0 && THREADS % PER == 0);
-    uint4 v[NL];
+    static_assert(COLS % VE == 0 && THREADS % PER == 0 && ROWS % STEP == 0);
+    u32x4 v[NL];
 
-    __device__ __forceinline__ void load(const T* src, uint32_t stride, int live, int cols)
+    __device__ __forceinline__ void load(const T* src, uint32_t stride, int live, int cols, bool near)
     {
         const int r0 = threadIdx.x / PER, c = (threadIdx.x % PER) * VE;
         if constexpr (VEC) {
-            const T* p = src + (c < cols ? c : 0);
+            const int c1 = c < cols ? c : 0;
+            if (live >= ROWS && near) {
+                const uint32_t off = (uint32_t)r0 * stride + (uint32_t)c1 * (uint32_t)sizeof(T);
 #pragma unroll
-            for (int n = 0; n < NL; ++n)
-                v[n] = *(const uint4*)row_at(p, min(r0 + n * STEP, live - 1), stride);
+                for (int n = 0; n < NL; ++n)
+                    v[n] = *(const u32x4*)((const char*)src + (uint64_t)(n * STEP) * stride + off);
+            } else {
+#pragma unroll
+                for (int n = 0; n < NL; ++n)
+                    v[n] = *(const u32x4*)row_at(src + c1, min(r0 + n * STEP, live - 1), stride);
+            }
         } else {
 #pragma unroll
             for (int n = 0; n < NL; ++n) {
@@ -160,23 +169,24 @@ template <typename D, typename El, int COLS, int THREADS, bool VEC, int ROWS = 6
                     if (c + j >= cols)
                         e[j] = D::put(0.0f);
                 }
-                v[n] = *(const uint4*)e;
+                v[n] = *(const u32x4*)e;
             }
         }
     }
     __device__ __forceinline__ void store(El* lds, int ld, int live, int cols)
     {
         const int r0 = threadIdx.x / PER, c = (threadIdx.x % PER) * VE;
+        El* d = lds + r0 * ld + c;
+        if (live >= ROWS && cols == COLS) {
 #pragma unroll
-        for (int n = 0; n < NL; ++n) {
-            const int r = r0 + n * STEP;
-            if (ROWS % STEP != 0 && r >= ROWS)
-                break;
-            const bool in = r < live && c < cols;
-            const uint4 w = {in ? v[n].x : 0, in ? v[n].y : 0, in ? v[n].z : 0, in ? v[n].w : 0};
-            El* d = lds + r * ld + c;
-            static_assert(sizeof(El) == sizeof(T));
-            *(uint4*)d = w;
+            for (int n = 0; n < NL; ++n)
+                *(u32x4*)(d + n * STEP * ld) = v[n];
+        } else {
+#pragma unroll
+            for (int n = 0; n < NL; ++n) {
+                const bool in = r0 + n * STEP < live && c < cols;
+                *(u32x4*)(d + n * STEP * ld) = u32x4{in ? v[n].x : 0, in ? v[n].y : 0, in ? v[n].z : 0, in ? v[n].w : 0};
+            }
         }
     }
 };
@@ -185,35 +195,94 @@ template <typename D, typename El, int COLS, int THREADS, bool VEC, int ROWS = 6
 // arrays; rows from `live` (>= 1) on become zeros
 template <typename El, int ROWS, int COLS, int THREADS> struct Dense {
     static constexpr int VE = 16 / sizeof(El), PER = COLS / VE, STEP = THREADS / PER, NL = (ROWS + STEP - 1) / STEP;
-    static_assert(THREADS % PER == 0);
-    uint4 v[NL];
+    static_assert(THREADS % PER == 0 && ROWS % STEP == 0);
+    u32x4 v[NL];
 
     __device__ __forceinline__ void load(const El* src, int live = ROWS)
     {
         const int r0 = threadIdx.x / PER, c = (threadIdx.x % PER) * VE;
+        if (live >= ROWS) {
+            const uint32_t off = (uint32_t)(r0 * COLS + c) * (uint32_t)sizeof(El);
 #pragma unroll
-        for (int n = 0; n < NL; ++n)
-            v[n] = *(const uint4*)(src + min(r0 + n * STEP, live - 1) * COLS + c);
+            for (int n = 0; n < NL; ++n)
+                v[n] = *(const u32x4*)((const char*)(src + n * STEP * COLS) + off);
+        } else {
+#pragma unroll
+            for (int n = 0; n < NL; ++n)
+                v[n] = *(const u32x4*)(src + min(r0 + n * STEP, live - 1) * COLS + c);
+        }
     }
     __device__ __forceinline__ void store(El* lds, int ld, int live = ROWS)
     {
         const int r0 = threadIdx.x / PER, c = (threadIdx.x % PER) * VE;
+        El* d = lds + r0 * ld + c;
+        if (live >= ROWS) {
 #pragma unroll
-        for (int n = 0; n < NL; ++n) {
-            const int r = r0 + n * STEP;
-            if (ROWS % STEP != 0 && r >= ROWS)
-                break;
-            const bool in = r < live;
-            *(uint4*)(lds + r * ld + c) = uint4{in ? v[n].x : 0, in ? v[n].y : 0, in ? v[n].z : 0, in ? v[n].w : 0};
+            for (int n = 0; n < NL; ++n)
+                *(u32x4*)(d + n * STEP * ld) = v[n];
+        } else {
+#pragma unroll
+            for (int n = 0; n < NL; ++n) {
+                const bool in = r0 + n * STEP < live;
+                *(u32x4*)(d + n * STEP * ld) = u32x4{in ? v[n].x : 0, in ? v[n].y : 0, in ? v[n].z : 0, in ? v[n].w : 0};
+            }
         }
     }
 };
+
+// A column's values at the steps of four result tiles (row 16 t + 4 g + r in
+// [t][r]); steps from `live` on give the last one's, whatever it holds
+template <typename T> struct Column {
+    T x[4][4];
+
+    __device__ __forceinline__ void load(const T* src, int v, uint32_t stride, int live, bool near)
+    {
+        const int g4 = 4 * ((threadIdx.x & 63) >> 4);
+        if (live >= 64 && near) {
+            const uint32_t off = (uint32_t)g4 * stride + (uint32_t)v * (uint32_t)sizeof(T);
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    x[t][r] = *(const T*)((const char*)src + (uint64_t)(16 * t + r) * stride + off);
+        } else {
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    x[t][r] = *row_at(src + v, min(16 * t + g4 + r, live - 1), stride);
+        }
+    }
+};
+
+// The reverse: steps below `live` are written
+template <typename D>
+__device__ __forceinline__ void store_column(const f32x4* x, typename D::T* dst, int v, uint32_t stride, int live, bool near)
+{
+    using T = typename D::T;
+    const int g4 = 4 * ((threadIdx.x & 63) >> 4);
+    if (live >= 64 && near) {
+        const uint32_t off = (uint32_t)g4 * stride + (uint32_t)v * (uint32_t)sizeof(T);
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                *(T*)((char*)dst + (uint64_t)(16 * t + r) * stride + off) = D::put(x[t][r]);
+    } else {
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                if (16 * t + g4 + r < live)
+                    *const_cast<T*>(row_at(dst + v, 16 * t + g4 + r, stride)) = D::put(x[t][r]);
+    }
+}
 
 // Four consecutive values of a result tile's column
 template <bool BF> __device__ __forceinline__ void put4(typename Mat<BF>::El* p, const f32x4 v)
 {
     if constexpr (BF)
-        *(bf16x4*)p = bf16x4{(__bf16)v[0], (__bf16)v[1], (__bf16)v[2], (__bf16)v[3]};
+        *(bf16x4*)p = __builtin_convertvector(v, bf16x4);
     else
         *(f32x4*)p = v;
 }
