@@ -102,8 +102,8 @@ __device__ void unit_lower_inverse(const float* A, float* X)
     if (wave < 2) {
         const int lo = 32 * wave, hi = lo + 16;
         f32x4 y = {0, 0, 0, 0}, z = {0, 0, 0, 0};
-        y = M::mma(M::rows(A + hi * LF + lo, LF, 0), M::cols(X + lo * LF + lo, LF, 0), y);
-        z = M::mma(M::rows(X + hi * LF + hi, LF, 0), y, z);
+        y = M::mma(M::rows_ld(A + hi * LF + lo, LF, 0, tid), M::cols_ld(X + lo * LF + lo, LF, 0, tid), y);
+        z = M::mma(M::rows_ld(X + hi * LF + hi, LF, 0, tid), y, z);
 #pragma unroll
         for (int r = 0; r < 4; ++r)
             X[(hi + 4 * g + r) * LF + lo + c] = -z[r];
@@ -117,11 +117,11 @@ __device__ void unit_lower_inverse(const float* A, float* X)
             y[i] = f32x4{0, 0, 0, 0};
 #pragma unroll
             for (int u = 0; u < 2; ++u)
-                y[i] = M::mma(M::rows(A + (32 + 16 * i) * LF, LF, u), M::cols(X + q, LF, u), y[i]);
+                y[i] = M::mma(M::rows_ld(A + (32 + 16 * i) * LF, LF, u, tid), M::cols_ld(X + q, LF, u, tid), y[i]);
         }
 #pragma unroll
         for (int u = 0; u < 2; ++u)
-            z = M::mma(M::rows(X + p * LF + 32, LF, u), y[u], z);
+            z = M::mma(M::rows_ld(X + p * LF + 32, LF, u, tid), y[u], z);
         // (rows 32.. of columns 0..31 are read by no wave here)
 #pragma unroll
         for (int r = 0; r < 4; ++r)
@@ -133,13 +133,12 @@ __device__ void unit_lower_inverse(const float* A, float* X)
 // X, P and the gates of a chunk, for the value heads of one key head
 template <bool BF, int DKP> struct PrepLds {
     using El = typename Mat<BF>::El;
-    static constexpr int LDK = DKP + Mat<BF>::PAD;
     union {
         struct {
-            El k[L * LDK], q[L * LDK];
+            Tile<El, L, DKP> k, q;
         };
         struct {  // (once the products of k and q are in registers)
-            float A[L * LF], X[L * LF];
+            alignas(16) float A[L * LF], X[L * LF];
         };
     };
     double G[L];
@@ -154,7 +153,7 @@ __global__ __launch_bounds__(256) void delta_prep(DeltaArgs a)
     using El = typename M::El;
     using Lds = PrepLds<BF, DKP>;
     __shared__ Lds s;
-    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, col = lane & 15, g4 = 4 * (lane >> 4);
+    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, col = lane & 15, g = lane >> 4;
     const int c = blockIdx.x % a.nc;
     const int64_t nh = blockIdx.x / a.nc;
     const int n = (int)(nh / a.Hk), hk = (int)(nh - (int64_t)n * a.Hk), group = a.Hv / a.Hk;
@@ -164,10 +163,10 @@ __global__ __launch_bounds__(256) void delta_prep(DeltaArgs a)
     const int64_t row0 = (int64_t)t0 * a.N + n;
     {
         Rows<D, El, DKP, 256, VEC> k, q;
-        k.load((const T*)a.k + row0 * a.k_row + (int64_t)hk * a.Dk, a.k_step, live, a.Dk, a.near);
-        q.load((const T*)a.q + row0 * a.q_row + (int64_t)hk * a.Dk, a.q_step, live, a.Dk, a.near);
-        k.store(s.k, Lds::LDK, live, a.Dk);
-        q.store(s.q, Lds::LDK, live, a.Dk);
+        k.load((const T*)a.k + row0 * a.k_row + (int64_t)hk * a.Dk, a.k_step, live, a.Dk, a.near, tid);
+        q.load((const T*)a.q + row0 * a.q_row + (int64_t)hk * a.Dk, a.q_step, live, a.Dk, a.near, tid);
+        k.store(s.k, live, a.Dk, tid);
+        q.store(s.q, live, a.Dk, tid);
     }
     __syncthreads();
     // (K K^T)[j][i] and (K Q^T)[j][i]: column i = 16 wave + col of every row tile j <= i
@@ -177,18 +176,18 @@ __global__ __launch_bounds__(256) void delta_prep(DeltaArgs a)
         kk[t] = kq[t] = f32x4{0, 0, 0, 0};
 #pragma unroll
     for (int u = 0; u < DKP / M::KU; ++u) {
-        const auto bk = M::rows(s.k + 16 * wave * Lds::LDK, Lds::LDK, u);
-        const auto bq = M::rows(s.q + 16 * wave * Lds::LDK, Lds::LDK, u);
+        const auto bk = M::rows(s.k, wave, u, tid);
+        const auto bq = M::rows(s.q, wave, u, tid);
 #pragma unroll
         for (int t = 0; t < 4; ++t)
-            if (t <= wave) {
-                const auto ak = M::rows(s.k + 16 * t * Lds::LDK, Lds::LDK, u);
+            if (M::reaches(t, wave)) {
+                const auto ak = M::rows(s.k, t, u, tid);
                 kk[t] = M::mma(ak, bk, kk[t]);
                 kq[t] = M::mma(ak, bq, kq[t]);
             }
     }
     __syncthreads();
-    const int i = 16 * wave + col;
+    const int i = M::at(wave, col >> 2) + (col & 3);
     for (int r = 0; r < group; ++r) {
         const int hv = hk * group + r;
         const int64_t unit = unit_of(a, n, hv, c);
@@ -208,9 +207,9 @@ __global__ __launch_bounds__(256) void delta_prep(DeltaArgs a)
         const double Gi = s.G[i];
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
-            const int j0 = 16 * t + g4;
+            const int j0 = M::at(t, g);
             f32x4 av = {0, 0, 0, 0}, pv = {0, 0, 0, 0};
-            if (t <= wave)
+            if (M::reaches(t, wave))
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const int j = j0 + e;
@@ -256,10 +255,9 @@ __global__ __launch_bounds__(256) void delta_prep(DeltaArgs a)
 // instructions hides a wave's latencies: operands are read a group ahead.
 template <bool BF, int DKP> struct ScanLds {
     using El = typename Mat<BF>::El;
-    static constexpr int LDK = DKP + Mat<BF>::PAD, LDL = L + Mat<BF>::PAD;
-    El k[L * LDK], q[L * LDK];
-    El x[BF ? 2 : 1][L * LDL], p[L * LDL];
-    float gate[3 * L];
+    Tile<El, L, DKP> k, q;
+    Tile<El, L, L> x[BF ? 2 : 1], p;
+    alignas(16) float gate[3 * L];
 };
 
 template <typename D, bool BF, int DKP, int NW, bool VEC>
@@ -273,7 +271,7 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(1, 1)))
     constexpr int TK = DKP / 16, TH = NW * 64, KU = M::KU, TU = M::TU, UK = DKP / KU, UL = L / KU;
     static_assert(TH >= 3 * L);
     __shared__ Lds s;
-    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, col = lane & 15, g4 = 4 * (lane >> 4);
+    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, col = lane & 15, g = lane >> 4;
     const int vblocks = (a.dvp + 16 * NW - 1) / (16 * NW);
     const int64_t head = blockIdx.x / vblocks;
     const int n = (int)(head / a.Hv), hv = (int)(head - (int64_t)n * a.Hv), hk = hv / (a.Hv / a.Hk);
@@ -286,37 +284,37 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(1, 1)))
     for (int t = 0; t < TK; ++t)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-            const int d = 16 * t + g4 + r;
+            const int d = M::at(t, g) + r;
             S[t][r] = a.state_in && mine && d < a.Dk ? a.state_in[(head * a.Dk + d) * a.Dv + v] : 0.0f;
         }
     Rows<D, El, DKP, TH, VEC> nk, nq;
     Dense<El, L, L, TH> nx[BF ? 2 : 1], np;
-    Column<T> nv;
+    Column<M, T> nv;
     float ngate;
-    const auto fetch = [&](int c) {
+    const auto fetch = [&](int c, int tid) {
         const int t0 = c * L, live = min(L, len - t0);
         const int64_t row0 = (int64_t)t0 * a.N + n, unit = unit_of(a, n, hv, c);
-        nk.load((const T*)a.k + row0 * a.k_row + (int64_t)hk * a.Dk, a.k_step, live, a.Dk, a.near);
-        nq.load((const T*)a.q + row0 * a.q_row + (int64_t)hk * a.Dk, a.q_step, live, a.Dk, a.near);
-        nx[0].load((const El*)a.X + unit * L * L * (BF ? 2 : 1));
+        nk.load((const T*)a.k + row0 * a.k_row + (int64_t)hk * a.Dk, a.k_step, live, a.Dk, a.near, tid);
+        nq.load((const T*)a.q + row0 * a.q_row + (int64_t)hk * a.Dk, a.q_step, live, a.Dk, a.near, tid);
+        nx[0].load((const El*)a.X + unit * L * L * (BF ? 2 : 1), L, tid);
         if constexpr (BF)
-            nx[1].load((const El*)a.X + unit * L * L * 2 + L * L);
-        np.load((const El*)a.P + unit * L * L);
-        nv.load((const T*)a.v + row0 * a.v_row + (int64_t)hv * a.Dv, mine ? v : 0, a.v_step, live, a.near);
+            nx[1].load((const El*)a.X + unit * L * L * 2 + L * L, L, tid);
+        np.load((const El*)a.P + unit * L * L, L, tid);
+        nv.load((const T*)a.v + row0 * a.v_row + (int64_t)hv * a.Dv, mine ? v : 0, a.v_step, live, a.near, tid);
         ngate = a.gate[unit * 3 * L + min(tid, 3 * L - 1)];
     };
     if (chunks > 0)
-        fetch(0);
+        fetch(0, tid);
     for (int c = 0; c < chunks; ++c) {
         const int t0 = c * L, live = min(L, len - t0);
         const int64_t row0 = (int64_t)t0 * a.N + n, unit = unit_of(a, n, hv, c);
         __syncthreads();
-        nk.store(s.k, Lds::LDK, live, a.Dk);
-        nq.store(s.q, Lds::LDK, live, a.Dk);
-        nx[0].store(s.x[0], Lds::LDL);
+        nk.store(s.k, live, a.Dk, tid);
+        nq.store(s.q, live, a.Dk, tid);
+        nx[0].store(s.x[0], L, tid);
         if constexpr (BF)
-            nx[1].store(s.x[1], Lds::LDL);
-        np.store(s.p, Lds::LDL);
+            nx[1].store(s.x[1], L, tid);
+        np.store(s.p, L, tid);
         if (tid < 3 * L)
             s.gate[tid] = ngate;
         f32x4 R[4];
@@ -328,16 +326,16 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(1, 1)))
             for (int t = 0; t < 4; ++t)
 #pragma unroll
                 for (int r = 0; r < 4; ++r)
-                    R[t][r] = mine && 16 * t + g4 + r < live ? R[t][r] : 0.0f;
+                    R[t][r] = mine && M::at(t, g) + r < live ? R[t][r] : 0.0f;
         }
         __syncthreads();
         if (c + 1 < chunks)
-            fetch(c + 1);
+            fetch(c + 1, again(threadIdx.x));
         if (a.S0 && wide) {  // [v][d], for the backward
-            El* S0 = (El*)a.S0 + (unit * a.dvp + v) * DKP;
+            El* S0 = (El*)a.S0 + (unit * a.dvp + v) * DKP + M::at(0, g);
 #pragma unroll
-            for (int t = 0; t < TK; ++t)
-                put4<BF>(S0 + 16 * t + g4, S[t]);
+            for (int u = 0; u < UK; ++u)
+                *(Frag*)(S0 + u * KU) = M::pack(S + u * TU);
         }
         // K S0 and Q S0.  16-bit: the state goes in as the sum of two numbers of 8 bits each.
         f32x4 KS[4], O[4], eG[4], sG[4], gam[4];
@@ -345,8 +343,8 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(1, 1)))
         const auto read_kq = [&](int u) {
 #pragma unroll
             for (int t = 0; t < 4; ++t) {
-                fk[u & 1][t] = M::rows(s.k + 16 * t * Lds::LDK, Lds::LDK, u);
-                fq[u & 1][t] = M::rows(s.q + 16 * t * Lds::LDK, Lds::LDK, u);
+                fk[u & 1][t] = M::rows(s.k, t, u, tid);
+                fq[u & 1][t] = M::rows(s.q, t, u, tid);
             }
         };
 #pragma unroll
@@ -361,18 +359,18 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(1, 1)))
             } else {
 #pragma unroll
                 for (int t = 0; t < 4; ++t) {
-                    eG[t] = *(const f32x4*)(s.gate + 16 * t + g4);
-                    sG[t] = *(const f32x4*)(s.gate + L + 16 * t + g4);
-                    gam[t] = *(const f32x4*)(s.gate + 2 * L + 16 * t + g4);
+                    eG[t] = *(const f32x4*)(s.gate + M::at(t, g));
+                    sG[t] = *(const f32x4*)(s.gate + L + M::at(t, g));
+                    gam[t] = *(const f32x4*)(s.gate + 2 * L + M::at(t, g));
                 }
 #pragma unroll
                 for (int w = 0; w < UL; ++w)
 #pragma unroll
                     for (int t = 0; t < 4; ++t)
-                        if (w * KU < 16 * (t + 1)) {  // (X and P are lower triangular)
-                            fx[w][t] = M::rows(s.x[0] + 16 * t * Lds::LDL, Lds::LDL, w);
+                        if (M::reaches(w * TU, t)) {  // (X and P are lower triangular)
+                            fx[w][t] = M::rows(s.x[0], t, w, tid);
                             if constexpr (BF)
-                                fl[w][t] = M::rows(s.x[1] + 16 * t * Lds::LDL, Lds::LDL, w);
+                                fl[w][t] = M::rows(s.x[1], t, w, tid);
                         }
             }
             in_order();
@@ -396,8 +394,8 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(1, 1)))
         for (int w = 0; w < UL; ++w)
 #pragma unroll
             for (int t = 0; t < 4; ++t)
-                if (w * KU < 16 * (t + 1))
-                    fp[w][t] = M::rows(s.p + 16 * t * Lds::LDL, Lds::LDL, w);
+                if (M::reaches(w * TU, t))
+                    fp[w][t] = M::rows(s.p, t, w, tid);
         in_order();
         // residuals r = X (V - diag(e^G) K S0)
         f32x4 U[4];
@@ -418,7 +416,7 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(1, 1)))
                 rest = M::pack_rest(R + u * TU, b);
 #pragma unroll
             for (int t = 0; t < 4; ++t)
-                if (u * KU < 16 * (t + 1)) {
+                if (M::reaches(u * TU, t)) {
                     U[t] = M::mma(fx[u][t], b, U[t]);
                     if constexpr (BF) {
                         U[t] = M::mma(fx[u][t], rest, U[t]);
@@ -429,16 +427,16 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(1, 1)))
         const auto read_kt = [&](int u) {
 #pragma unroll
             for (int t = 0; t < TK; ++t)
-                ft[u & 1][t] = M::cols(s.k + 16 * t, Lds::LDK, u);
+                ft[u & 1][t] = M::cols(s.k, t, u, tid);
         };
         in_order();
         read_kt(0);
         in_order();
         if (a.U && wide) {  // [v][i]
-            El* pu = (El*)a.U + (unit * a.dvp + v) * L;
+            El* pu = (El*)a.U + (unit * a.dvp + v) * L + M::at(0, g);
 #pragma unroll
-            for (int t = 0; t < 4; ++t)
-                put4<BF>(pu + 16 * t + g4, U[t]);
+            for (int u = 0; u < UL; ++u)
+                *(Frag*)(pu + u * KU) = M::pack(U + u * TU);
         }
         // outputs
 #pragma unroll
@@ -446,13 +444,13 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(1, 1)))
             const Frag b = M::pack(U + u * TU);
 #pragma unroll
             for (int t = 0; t < 4; ++t)
-                if (u * KU < 16 * (t + 1))
+                if (M::reaches(u * TU, t))
                     O[t] = M::mma(fp[u][t], b, O[t]);
             if constexpr (BF) {
                 const Frag rest = M::pack_rest(U + u * TU, b);
 #pragma unroll
                 for (int t = 0; t < 4; ++t)
-                    if (u * KU < 16 * (t + 1))
+                    if (M::reaches(u * TU, t))
                         O[t] = M::mma(fp[u][t], rest, O[t]);
             }
         }
@@ -486,7 +484,7 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(1, 1)))
             in_order();
         }
         if (mine)
-            store_column<D>(O, (T*)a.o + (row0 * a.Hv + hv) * a.Dv, v, a.o_step, live, a.near);
+            store_column<M, D>(O, (T*)a.o + (row0 * a.Hv + hv) * a.Dv, v, a.o_step, live, a.near, again(threadIdx.x));
     }
     if (!mine)
         return;
@@ -497,7 +495,7 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(1, 1)))
         for (int t = 0; t < TK; ++t)
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                const int d = 16 * t + g4 + r;
+                const int d = M::at(t, g) + r;
                 if (d < a.Dk)
                     a.state_out[(head * a.Dk + d) * a.Dv + v] = S[t][r];
             }
@@ -507,9 +505,9 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(1, 1)))
 // values' gradient
 template <bool BF, int DKP> struct RscanLds {
     using El = typename Mat<BF>::El;
-    static constexpr int LDK = DKP + Mat<BF>::PAD, LDL = L + Mat<BF>::PAD;
-    El k[L * LDK], q[L * LDK], x[L * LDL], p[L * LDL];
-    float gate[3 * L];
+    Tile<El, L, DKP> k, q;
+    Tile<El, L, L> x, p;
+    alignas(16) float gate[3 * L];
 };
 
 template <typename D, bool BF, int DKP, int NW, bool VEC>
@@ -523,7 +521,7 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(1, 1)))
     constexpr int TK = DKP / 16, TH = NW * 64, KU = M::KU, TU = M::TU, UK = DKP / KU, UL = L / KU;
     static_assert(TH >= 3 * L);
     __shared__ Lds s;
-    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, col = lane & 15, g4 = 4 * (lane >> 4);
+    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, col = lane & 15, g = lane >> 4;
     const int vblocks = (a.dvp + 16 * NW - 1) / (16 * NW);
     const int64_t head = blockIdx.x / vblocks;
     const int n = (int)(head / a.Hv), hv = (int)(head - (int64_t)n * a.Hv), hk = hv / (a.Hv / a.Hk);
@@ -535,33 +533,33 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(1, 1)))
     for (int t = 0; t < TK; ++t)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-            const int d = 16 * t + g4 + r;
+            const int d = M::at(t, g) + r;
             S[t][r] = a.grad_state_out && mine && d < a.Dk ? a.grad_state_out[(head * a.Dk + d) * a.Dv + v] : 0.0f;
         }
     Rows<D, El, DKP, TH, VEC> nk, nq;
     Dense<El, L, L, TH> nx, np;
-    Column<T> no;
+    Column<M, T> no;
     float ngate;
-    const auto fetch = [&](int c) {
+    const auto fetch = [&](int c, int tid) {
         const int t0 = c * L, live = min(L, len - t0);
         const int64_t row0 = (int64_t)t0 * a.N + n, unit = unit_of(a, n, hv, c);
-        nk.load((const T*)a.k + row0 * a.k_row + (int64_t)hk * a.Dk, a.k_step, live, a.Dk, a.near);
-        nq.load((const T*)a.q + row0 * a.q_row + (int64_t)hk * a.Dk, a.q_step, live, a.Dk, a.near);
-        nx.load((const El*)a.X + unit * L * L * (BF ? 2 : 1));
-        np.load((const El*)a.P + unit * L * L);
-        no.load((const T*)a.grad_o + (row0 * a.Hv + hv) * a.Dv, mine ? v : 0, a.o_step, live, a.near);
+        nk.load((const T*)a.k + row0 * a.k_row + (int64_t)hk * a.Dk, a.k_step, live, a.Dk, a.near, tid);
+        nq.load((const T*)a.q + row0 * a.q_row + (int64_t)hk * a.Dk, a.q_step, live, a.Dk, a.near, tid);
+        nx.load((const El*)a.X + unit * L * L * (BF ? 2 : 1), L, tid);
+        np.load((const El*)a.P + unit * L * L, L, tid);
+        no.load((const T*)a.grad_o + (row0 * a.Hv + hv) * a.Dv, mine ? v : 0, a.o_step, live, a.near, tid);
         ngate = a.gate[unit * 3 * L + min(tid, 3 * L - 1)];
     };
     if (chunks > 0)
-        fetch(chunks - 1);
+        fetch(chunks - 1, tid);
     for (int c = chunks - 1; c >= 0; --c) {
         const int t0 = c * L, live = min(L, len - t0);
         const int64_t row0 = (int64_t)t0 * a.N + n, unit = unit_of(a, n, hv, c);
         __syncthreads();
-        nk.store(s.k, Lds::LDK, live, a.Dk);
-        nq.store(s.q, Lds::LDK, live, a.Dk);
-        nx.store(s.x, Lds::LDL);
-        np.store(s.p, Lds::LDL);
+        nk.store(s.k, live, a.Dk, tid);
+        nq.store(s.q, live, a.Dk, tid);
+        nx.store(s.x, L, tid);
+        np.store(s.p, L, tid);
         if (tid < 3 * L)
             s.gate[tid] = ngate;
         f32x4 dO[4];
@@ -573,16 +571,16 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(1, 1)))
             for (int t = 0; t < 4; ++t)
 #pragma unroll
                 for (int r = 0; r < 4; ++r)
-                    dO[t][r] = mine && 16 * t + g4 + r < live ? dO[t][r] : 0.0f;
+                    dO[t][r] = mine && M::at(t, g) + r < live ? dO[t][r] : 0.0f;
         }
         __syncthreads();
         if (c > 0)
-            fetch(c - 1);
+            fetch(c - 1, again(threadIdx.x));
         if (wide) {  // [v][d], for delta_grads
-            El* dS = (El*)a.dS + (unit * a.dvp + v) * DKP;
+            El* dS = (El*)a.dS + (unit * a.dvp + v) * DKP + M::at(0, g);
 #pragma unroll
-            for (int t = 0; t < TK; ++t)
-                put4<BF>(dS + 16 * t + g4, S[t]);
+            for (int u = 0; u < UK; ++u)
+                *(Frag*)(dS + u * KU) = M::pack(S + u * TU);
         }
         // dr' = diag(e^{G_last - G} beta) K dS1 + P^T dO
         f32x4 R[4], eG[4], sG[4], gam[4];
@@ -590,7 +588,7 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(1, 1)))
         const auto read_k = [&](int u) {
 #pragma unroll
             for (int t = 0; t < 4; ++t)
-                fk[u & 1][t] = M::rows(s.k + 16 * t * Lds::LDK, Lds::LDK, u);
+                fk[u & 1][t] = M::rows(s.k, t, u, tid);
         };
 #pragma unroll
         for (int t = 0; t < 4; ++t)
@@ -604,16 +602,16 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(1, 1)))
             } else {
 #pragma unroll
                 for (int t = 0; t < 4; ++t) {
-                    eG[t] = *(const f32x4*)(s.gate + 16 * t + g4);
-                    sG[t] = *(const f32x4*)(s.gate + L + 16 * t + g4);
-                    gam[t] = *(const f32x4*)(s.gate + 2 * L + 16 * t + g4);
+                    eG[t] = *(const f32x4*)(s.gate + M::at(t, g));
+                    sG[t] = *(const f32x4*)(s.gate + L + M::at(t, g));
+                    gam[t] = *(const f32x4*)(s.gate + 2 * L + M::at(t, g));
                 }
 #pragma unroll
                 for (int w = 0; w < UL; ++w)
 #pragma unroll
                     for (int t = 0; t < 4; ++t)
-                        if ((w + 1) * KU > 16 * t)  // (transposed: upper triangular)
-                            fp[w][t] = M::cols(s.p + 16 * t, Lds::LDL, w);
+                        if (M::reaches(t, w * TU))  // (transposed: upper triangular)
+                            fp[w][t] = M::cols(s.p, t, w, tid);
             }
             in_order();
             const Frag b = M::pack(S + u * TU);
@@ -626,12 +624,12 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(1, 1)))
         for (int w = 0; w < UL; ++w)
 #pragma unroll
             for (int t = 0; t < 4; ++t)
-                if ((w + 1) * KU > 16 * t)
-                    fx[w][t] = M::cols(s.x + 16 * t, Lds::LDL, w);
-        const auto read_t = [&](const El* tile, int u) {
+                if (M::reaches(t, w * TU))
+                    fx[w][t] = M::cols(s.x, t, w, tid);
+        const auto read_t = [&](const Tile<El, L, DKP>& tile, int u) {
 #pragma unroll
             for (int t = 0; t < TK; ++t)
-                ft[u & 1][t] = M::cols(tile + 16 * t, Lds::LDK, u);
+                ft[u & 1][t] = M::cols(tile, t, u, tid);
         };
         read_t(s.q, 0);
         in_order();
@@ -645,7 +643,7 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(1, 1)))
             const Frag b = M::pack(dO + u * TU);
 #pragma unroll
             for (int t = 0; t < 4; ++t)
-                if ((u + 1) * KU > 16 * t)
+                if (M::reaches(t, u * TU))
                     R[t] = M::mma(fp[u][t], b, R[t]);
         }
         // dV = X^T dr', and meanwhile dS0 = e^{G_last} dS1 + scale Q^T diag(e^G) dO - K^T diag(e^G) dV
@@ -681,11 +679,11 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(1, 1)))
             const Frag b = M::pack(R + u * TU);
 #pragma unroll
             for (int t = 0; t < 4; ++t)
-                if ((u + 1) * KU > 16 * t)
+                if (M::reaches(t, u * TU))
                     dV[t] = M::mma(fx[u][t], b, dV[t]);
         }
         if (mine)
-            store_column<D>(dV, (T*)a.grad_v + (row0 * a.Hv + hv) * a.Dv, v, a.o_step, live, a.near);
+            store_column<M, D>(dV, (T*)a.grad_v + (row0 * a.Hv + hv) * a.Dv, v, a.o_step, live, a.near, again(threadIdx.x));
 #pragma unroll
         for (int t = 0; t < 4; ++t)
 #pragma unroll
@@ -712,7 +710,7 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(1, 1)))
         for (int t = 0; t < TK; ++t)
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                const int d = 16 * t + g4 + r;
+                const int d = M::at(t, g) + r;
                 if (d < a.Dk)
                     a.grad_state_in[(head * a.Dk + d) * a.Dv + v] = S[t][r];
             }
@@ -727,22 +725,25 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(1, 1)))
 template <bool BF, int DKP> struct GradsLds {
     using El = typename Mat<BF>::El;
     static constexpr int VB = BF ? 64 : 32;  // values staged at a time
-    static constexpr int LDK = DKP + Mat<BF>::PAD, LDL = L + Mat<BF>::PAD, LDV = VB + Mat<BF>::PAD;
-    El k[L * LDK], q[L * LDK];
+    Tile<El, L, DKP> k, q;
     union {
         struct {
-            El dO[L * LDV], dV[L * LDV], r[VB * LDL], S0[VB * LDK], dS[VB * LDK];
+            Tile<El, L, VB> dO, dV;
+            Tile<El, VB, L> r;
+            Tile<El, VB, DKP> S0, dS;
         } v;
-        El EF[2][L * LDL];  // [i][j]
+        Tile<El, L, L> EF[2];  // [i][j]
     };
     double G[L];
     float eG[L], to_end[L], beta[L];
-    float sum[8][L];                             // over a wave's steps i > j, of each step j
+    alignas(16) float sum[8][L];                             // over a wave's steps i > j, of each step j
     float a[2][L], x[2][L], row[2][L], diag[L];  // of each step
     float z[8];
 };
 
-template <typename D, bool BF, int DKP, bool VEC>
+// ONE: every key head has one value head (nothing is summed over heads, so the
+// sums need no registers of their own while a head is computed)
+template <typename D, bool BF, int DKP, bool VEC, bool ONE>
 __global__ __launch_bounds__(512) void delta_grads(DeltaArgs a)
 {
     using T = typename D::T;
@@ -752,38 +753,39 @@ __global__ __launch_bounds__(512) void delta_grads(DeltaArgs a)
     using Lds = GradsLds<BF, DKP>;
     constexpr int TH = DKP / 32, KU = M::KU, UK = DKP / KU, UL = L / KU, VB = Lds::VB;
     __shared__ Lds s;
-    const int tid = threadIdx.x, wave8 = tid >> 6, lane = tid & 63, col = lane & 15, g4 = 4 * (lane >> 4);
-    const int wave = wave8 & 3, half = wave8 >> 2, d0 = half * (DKP / 2);
+    const int tid = threadIdx.x, wave8 = tid >> 6, lane = tid & 63, col = lane & 15, g = lane >> 4;
+    const int wave = wave8 & 3, half = wave8 >> 2;
     const int c = blockIdx.x % a.nc;
     const int64_t nh = blockIdx.x / a.nc;
-    const int n = (int)(nh / a.Hk), hk = (int)(nh - (int64_t)n * a.Hk), group = a.Hv / a.Hk;
+    const int n = (int)(nh / a.Hk), hk = (int)(nh - (int64_t)n * a.Hk), group = ONE ? 1 : a.Hv / a.Hk;
     const int t0 = c * L, live = max(0, min(L, length_of(a, n) - t0)), steps = min(L, a.T - t0);
     const int64_t row0 = (int64_t)t0 * a.N + n;
-    const int i = 16 * wave + col;
+    const int i = M::at(wave, col >> 2) + (col & 3);
     f32x4 dq[TH], dk[TH];
 #pragma unroll
     for (int t = 0; t < TH; ++t)
         dq[t] = dk[t] = f32x4{0, 0, 0, 0};
     if (live > 0) {
         Rows<D, El, DKP, 512, VEC> nk, nq;
-        nk.load((const T*)a.k + row0 * a.k_row + (int64_t)hk * a.Dk, a.k_step, live, a.Dk, a.near);
-        nq.load((const T*)a.q + row0 * a.q_row + (int64_t)hk * a.Dk, a.q_step, live, a.Dk, a.near);
+        nk.load((const T*)a.k + row0 * a.k_row + (int64_t)hk * a.Dk, a.k_step, live, a.Dk, a.near, tid);
+        nq.load((const T*)a.q + row0 * a.q_row + (int64_t)hk * a.Dk, a.q_step, live, a.Dk, a.near, tid);
         for (int h = 0; h < group; ++h) {
+            const int tid = again(threadIdx.x);
             const int hv = hk * group + h;
             const int64_t unit = unit_of(a, n, hv, c);
             Rows<D, El, VB, 512, VEC> no, nd;
             Dense<El, VB, L, 512> nr;
             Dense<El, VB, DKP, 512> n0, n1;
-            const auto fetch = [&](int v0) {
+            const auto fetch = [&](int v0, int tid) {
                 const int rows = min(VB, a.dvp - v0), cols = min(VB, a.Dv - v0);
                 const int64_t at = (row0 * a.Hv + hv) * a.Dv + v0;
-                no.load((const T*)a.grad_o + at, a.o_step, live, cols, a.near);
-                nd.load((const T*)a.grad_v + at, a.o_step, live, cols, a.near);
-                nr.load((const El*)a.U + (unit * a.dvp + v0) * L, rows);
-                n0.load((const El*)a.S0 + (unit * a.dvp + v0) * DKP, rows);
-                n1.load((const El*)a.dS + (unit * a.dvp + v0) * DKP, rows);
+                no.load((const T*)a.grad_o + at, a.o_step, live, cols, a.near, tid);
+                nd.load((const T*)a.grad_v + at, a.o_step, live, cols, a.near, tid);
+                nr.load((const El*)a.U + (unit * a.dvp + v0) * L, rows, tid);
+                n0.load((const El*)a.S0 + (unit * a.dvp + v0) * DKP, rows, tid);
+                n1.load((const El*)a.dS + (unit * a.dvp + v0) * DKP, rows, tid);
             };
-            fetch(0);
+            fetch(0, tid);
             if (wave8 == 0) {
                 const int64_t at = (row0 + (int64_t)min(lane, live - 1) * a.N) * a.Hv + hv;
                 const float gv = D::get(((const T*)a.g)[at]), bv = D::get(((const T*)a.beta)[at]);
@@ -803,32 +805,33 @@ __global__ __launch_bounds__(512) void delta_grads(DeltaArgs a)
                 dX[t] = f32x4{0, 0, 0, 0};
             float z = 0.0f;  // <S0, dS1>
             for (int v0 = 0; v0 < a.dvp; v0 += VB) {
+                const int tid = again(threadIdx.x);
                 const int rows = min(VB, a.dvp - v0), cols = min(VB, a.Dv - v0);
                 __syncthreads();
                 if (h == 0 && v0 == 0) {
-                    nk.store(s.k, Lds::LDK, live, a.Dk);
-                    nq.store(s.q, Lds::LDK, live, a.Dk);
+                    nk.store(s.k, live, a.Dk, tid);
+                    nq.store(s.q, live, a.Dk, tid);
                 }
-                no.store(s.v.dO, Lds::LDV, live, cols);
-                nd.store(s.v.dV, Lds::LDV, live, cols);
-                nr.store(s.v.r, Lds::LDL, rows);
-                n0.store(s.v.S0, Lds::LDK, rows);
-                n1.store(s.v.dS, Lds::LDK, rows);
+                no.store(s.v.dO, live, cols, tid);
+                nd.store(s.v.dV, live, cols, tid);
+                nr.store(s.v.r, rows, tid);
+                n0.store(s.v.S0, rows, tid);
+                n1.store(s.v.dS, rows, tid);
                 __syncthreads();
                 if (v0 + VB < a.dvp)
-                    fetch(v0 + VB);
+                    fetch(v0 + VB, tid);
 #pragma unroll
                 for (int u = 0; u < VB / KU; ++u) {
-                    const Frag bo = M::rows(s.v.dO + 16 * wave * Lds::LDV, Lds::LDV, u);
-                    const Frag bv = M::rows(s.v.dV + 16 * wave * Lds::LDV, Lds::LDV, u);
-                    const Frag br = M::cols(s.v.r + 16 * wave, Lds::LDL, u);
+                    const Frag bo = M::rows(s.v.dO, wave, u, tid);
+                    const Frag bv = M::rows(s.v.dV, wave, u, tid);
+                    const Frag br = M::cols(s.v.r, wave, u, tid);
                     Frag ar[4], as[TH];
 #pragma unroll
                     for (int t = 0; t < TH; ++t)
-                        as[t] = M::cols(s.v.S0 + d0 + 16 * t, Lds::LDK, u);
+                        as[t] = M::cols(s.v.S0, half * TH + t, u, tid);
 #pragma unroll
                     for (int t = 0; t < 4; ++t)
-                        ar[t] = M::cols(s.v.r + 16 * t, Lds::LDL, u);
+                        ar[t] = M::cols(s.v.r, t, u, tid);
                     in_order();
 #pragma unroll
                     for (int t = 0; t < TH; ++t) {
@@ -838,12 +841,12 @@ __global__ __launch_bounds__(512) void delta_grads(DeltaArgs a)
                     in_order();
 #pragma unroll
                     for (int t = 0; t < TH; ++t)
-                        as[t] = M::cols(s.v.dS + d0 + 16 * t, Lds::LDK, u);
+                        as[t] = M::cols(s.v.dS, half * TH + t, u, tid);
                     in_order();
                     const Frag bx = half ? bv : bo;
 #pragma unroll
                     for (int t = 0; t < 4; ++t)
-                        if (t <= wave)
+                        if (M::reaches(t, wave))
                             dX[t] = M::mma(ar[t], bx, dX[t]);
 #pragma unroll
                     for (int t = 0; t < TH; ++t)
@@ -852,8 +855,8 @@ __global__ __launch_bounds__(512) void delta_grads(DeltaArgs a)
                 }
 #pragma unroll
                 for (int e = tid * 4; e < VB * DKP; e += 2048) {
-                    const El* p0 = s.v.S0 + (e / DKP) * Lds::LDK + e % DKP;
-                    const El* p1 = s.v.dS + (e / DKP) * Lds::LDK + e % DKP;
+                    const int at = s.v.S0.off(e / DKP, e % DKP);
+                    const El *p0 = s.v.S0.e + at, *p1 = s.v.dS.e + at;
 #pragma unroll
                     for (int j = 0; j < 4; ++j)
                         z = __builtin_fmaf(M::get(p0[j]), M::get(p1[j]), z);
@@ -865,19 +868,20 @@ __global__ __launch_bounds__(512) void delta_grads(DeltaArgs a)
 #pragma unroll
             for (int t = 0; t < 4; ++t)
                 kx[t] = f32x4{0, 0, 0, 0};
-            const El* other = half ? s.k : s.q;
+            const Tile<El, L, DKP>& other = half ? s.k : s.q;
 #pragma unroll
             for (int u = 0; u < UK; ++u) {
-                const Frag b = M::rows(other + 16 * wave * Lds::LDK, Lds::LDK, u);
+                const Frag b = M::rows(other, wave, u, tid);
                 Frag ak[4];
 #pragma unroll
                 for (int t = 0; t < 4; ++t)
-                    ak[t] = M::rows(s.k + 16 * t * Lds::LDK, Lds::LDK, u);
+                    ak[t] = M::rows(s.k, t, u, tid);
                 in_order();
 #pragma unroll
                 for (int t = 0; t < 4; ++t)
-                    if (t <= wave)
+                    if (M::reaches(t, wave))
                         kx[t] = M::mma(ak[t], b, kx[t]);
+                in_order();
             }
             // E^T (first half) or F^T in place of the products; sums over i and over j of E q.k, F k.k
             const double Gi = s.G[i];
@@ -885,10 +889,10 @@ __global__ __launch_bounds__(512) void delta_grads(DeltaArgs a)
 #pragma unroll
             for (int t = 0; t < 4; ++t) {
                 f32x4 y = {0, 0, 0, 0}, w = {0, 0, 0, 0};
-                if (t <= wave) {
+                if (M::reaches(t, wave)) {
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        const int j = 16 * t + g4 + e;
+                        const int j = M::at(t, g) + e;
                         const float m = j <= i - half ? expf((float)(Gi - s.G[j])) : 0.0f;
                         const float f = (half ? -m : a.scale * m) * dX[t][e], b = s.beta[j], both = f * kx[t][e];
                         y[e] = j < i ? both : 0.0f;
@@ -903,16 +907,17 @@ __global__ __launch_bounds__(512) void delta_grads(DeltaArgs a)
                             y[e] += __shfl_xor(y[e], o);
                 }
                 if (col == 0)
-                    *(f32x4*)(s.sum[wave8] + 16 * t + g4) = y;
-                put4<BF>(s.EF[half] + i * Lds::LDL + 16 * t + g4, w);
+                    *(f32x4*)(s.sum[wave8] + M::at(t, g)) = y;
+                put4<BF>(s.EF[half].e + s.EF[half].off(i, M::at(t, g)), w);
+                in_order();
             }
             // products with the states, and what the gates take of them
             float ra = 0.0f, rx = 0.0f;
             const float eG = s.eG[i], to_end = s.to_end[i], bi = s.beta[i];
 #pragma unroll
             for (int t = 0; t < TH; ++t) {
-                const El* pk = s.k + i * Lds::LDK + d0 + 16 * t + g4;
-                const El* pq = s.q + i * Lds::LDK + d0 + 16 * t + g4;
+                const int at = Tile<El, L, DKP>::off(i, M::at(half * TH + t, g));
+                const El *pk = s.k.e + at, *pq = s.q.e + at;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const float kd = M::get(pk[e]), qd = M::get(pq[e]);
@@ -922,6 +927,7 @@ __global__ __launch_bounds__(512) void delta_grads(DeltaArgs a)
                     dq[t][e] += dq1;
                     dk[t][e] += bi * dk2 - dk1;
                 }
+                in_order();
             }
 #pragma unroll
             for (int o = 16; o < 64; o <<= 1) {
@@ -945,14 +951,14 @@ __global__ __launch_bounds__(512) void delta_grads(DeltaArgs a)
             __syncthreads();
 #pragma unroll
             for (int u = 0; u < UL; ++u) {
-                const Frag bE = M::rows(s.EF[0] + 16 * wave * Lds::LDL, Lds::LDL, u);
-                const Frag bF = M::rows(s.EF[1] + 16 * wave * Lds::LDL, Lds::LDL, u);
-                const Frag cE = M::cols(s.EF[0] + 16 * wave, Lds::LDL, u), cF = M::cols(s.EF[1] + 16 * wave, Lds::LDL, u);
+                const Frag bE = M::rows(s.EF[0], wave, u, tid);
+                const Frag bF = M::rows(s.EF[1], wave, u, tid);
+                const Frag cE = M::cols(s.EF[0], wave, u, tid), cF = M::cols(s.EF[1], wave, u, tid);
                 Frag ak[TH], aq[TH];
 #pragma unroll
                 for (int t = 0; t < TH; ++t) {
-                    ak[t] = M::cols(s.k + d0 + 16 * t, Lds::LDK, u);
-                    aq[t] = M::cols(s.q + d0 + 16 * t, Lds::LDK, u);
+                    ak[t] = M::cols(s.k, half * TH + t, u, tid);
+                    aq[t] = M::cols(s.q, half * TH + t, u, tid);
                 }
                 in_order();
 #pragma unroll
@@ -1000,7 +1006,7 @@ __global__ __launch_bounds__(512) void delta_grads(DeltaArgs a)
         T* pk = (T*)a.grad_k + at;
 #pragma unroll
         for (int t = 0; t < TH; ++t) {
-            const int d = d0 + 16 * t + g4;
+            const int d = M::at(half * TH + t, g);
             if (i >= live)
                 dq[t] = dk[t] = f32x4{0, 0, 0, 0};
             if (VEC) {  // (Dk is a multiple of 4 and the rows are aligned to them)
@@ -1042,7 +1048,11 @@ template <typename D, bool BF, int DKP, bool VEC> hipError_t backward(const Delt
     const hipError_t err = hipGetLastError();
     if (err != hipSuccess || a.nc == 0)
         return err;
-    delta_grads<D, BF, DKP, VEC><<<dim3((unsigned)((int64_t)a.N * a.Hk * a.nc)), dim3(512), 0, s>>>(a);
+    const dim3 grid((unsigned)((int64_t)a.N * a.Hk * a.nc));
+    if (a.Hk == a.Hv)
+        delta_grads<D, BF, DKP, VEC, true><<<grid, dim3(512), 0, s>>>(a);
+    else
+        delta_grads<D, BF, DKP, VEC, false><<<grid, dim3(512), 0, s>>>(a);
     return hipGetLastError();
 }
 

@@ -8,16 +8,30 @@
 // the same.  So the order is chosen such that a result's registers are a
 // right operand as they are: f32 contracts one tile's 16 rows in four
 // v_mfma_f32_16x16x4_f32, number r over the rows {4 g + r}; bf16 contracts two
-// tiles' 32 rows in one v_mfma_f32_16x16x32_bf16, lane group g over the rows
-// 4 g .. 4 g + 3 of the first tile, then those of the second.  A chain of
-// products (state -> residuals -> values -> state) then needs no LDS round
-// trip and no barrier.
+// tiles' 32 rows in one v_mfma_f32_16x16x32_bf16, lane group g over the first
+// tile's rows 4 g .. 4 g + 3, then the second's.  A chain of products (state ->
+// residuals -> values -> state) then needs no LDS round trip and no barrier.
+// Which index a tile's row stands for is free as well: bf16 tiles 2 u and
+// 2 u + 1 have 32 u + 8 g + r and 32 u + 8 g + 4 + r in their rows 4 g + r
+// (Mat::at), so that a lane's eight contraction indices are neighbours in
+// memory: left operands are read 16 bytes at a time, results stored so.
 #pragma once
 
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
 namespace mfpsn {
+
+// The same value, not known to be: what is computed from it is computed anew.
+// The functions below take the thread's index as an argument, and the kernels
+// give them again(threadIdx.x) of each pass through a loop: known as one value,
+// all of the loop's addresses are computed before it and kept, which took over
+// 100 registers (and spilled as many).
+__device__ __forceinline__ int again(int t)
+{
+    asm volatile("" : "+v"(t));
+    return t;
+}
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
@@ -41,19 +55,33 @@ template <> struct Mat<false> {
     using Frag = f32x4;
     static constexpr int KU = 16;   // rows that one product contracts
     static constexpr int TU = 1;    // result tiles that make one right operand
-    static constexpr int PAD = 4;   // elements between the rows of an LDS tile: rows start 4 banks apart
-    // operand from LDS [m][k]: rows m0 .. m0 + 15 (p points at row m0), contraction block u
-    __device__ static Frag rows(const El* p, int ld, int u)
+    // index of row 4 g of tile t
+    __device__ static constexpr int at(int t, int g) { return 16 * t + 4 * g; }
+    // whether tile t has rows at or before the last of tile w
+    __device__ static constexpr bool reaches(int t, int w) { return t <= w; }
+    // operands from padded rows: [m][k] of 16 rows m, contraction block u; [k][m]
+    __device__ static Frag rows_ld(const El* p, int ld, int u, int tid)
     {
-        const int lane = threadIdx.x & 63;
+        const int lane = tid & 63;
         return *(const f32x4*)(p + (lane & 15) * ld + 16 * u + 4 * (lane >> 4));
     }
-    // operand from LDS [k][m]: columns 0 .. 15 of p
-    __device__ static Frag cols(const El* p, int ld, int u)
+    __device__ static Frag cols_ld(const El* p, int ld, int u, int tid)
     {
-        const int lane = threadIdx.x & 63;
+        const int lane = tid & 63;
         const El* s = p + (16 * u + 4 * (lane >> 4)) * ld + (lane & 15);
         return f32x4{s[0], s[ld], s[2 * ld], s[3 * ld]};
+    }
+    // operand from an LDS tile [m][k]: row tile t, contraction block u
+    template <typename Tile> __device__ static Frag rows(const Tile& s, int t, int u, int tid)
+    {
+        const int lane = tid & 63;
+        return *(const f32x4*)(s.e + Tile::off(16 * t + (lane & 15), 16 * u + 4 * (lane >> 4)));
+    }
+    // operand from an LDS tile [k][m]: column tile t, contraction block u
+    template <typename Tile> __device__ static Frag cols(const Tile& s, int t, int u, int tid)
+    {
+        const int lane = tid & 63, k = 16 * u + 4 * (lane >> 4), m = 16 * t + (lane & 15);
+        return f32x4{s.e[Tile::off(k, m)], s.e[Tile::off(k + 1, m)], s.e[Tile::off(k + 2, m)], s.e[Tile::off(k + 3, m)]};
     }
     __device__ static Frag pack(const f32x4* t) { return t[0]; }
     __device__ static f32x4 mma(Frag a, Frag b, f32x4 c) { return mfma_f32(a, b, c); }
@@ -64,13 +92,14 @@ template <> struct Mat<false> {
 template <> struct Mat<true> {
     using El = __bf16;
     using Frag = bf16x8;
-    static constexpr int KU = 32, TU = 2, PAD = 8;
+    static constexpr int KU = 32, TU = 2;
     __device__ static Frag join(bf16x4 a, bf16x4 b) { return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7); }
-    __device__ static Frag rows(const El* p, int ld, int u)
+    __device__ static constexpr int at(int t, int g) { return 32 * (t >> 1) + 8 * g + 4 * (t & 1); }
+    __device__ static constexpr bool reaches(int t, int w) { return t >> 1 <= w >> 1; }
+    template <typename Tile> __device__ static Frag rows(const Tile& s, int t, int u, int tid)
     {
-        const int lane = threadIdx.x & 63;
-        const El* s = p + (lane & 15) * ld + 32 * u + 4 * (lane >> 4);
-        return join(*(const bf16x4*)s, *(const bf16x4*)(s + 16));
+        const int lane = tid & 63;
+        return *(const bf16x8*)(s.e + Tile::off(at(t, (lane & 15) >> 2) + (lane & 3), 32 * u + 8 * (lane >> 4)));
     }
     // 16 lanes read 4 rows of 16 columns, 8 bytes each, and get a column's 4 rows each
     __device__ static bf16x4 transposed(const El* p)
@@ -78,11 +107,10 @@ template <> struct Mat<true> {
         const i16x4 v = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4*)p);
         return __builtin_bit_cast(bf16x4, v);
     }
-    __device__ static Frag cols(const El* p, int ld, int u)
+    template <typename Tile> __device__ static Frag cols(const Tile& s, int t, int u, int tid)
     {
-        const int lane = threadIdx.x & 63, i = lane & 15;
-        const El* s = p + (32 * u + 4 * (lane >> 4) + (i >> 2)) * ld + 4 * (i & 3);
-        return join(transposed(s), transposed(s + 16 * ld));
+        const int lane = tid & 63, i = lane & 15, k = 32 * u + 8 * (lane >> 4) + (i >> 2), m = at(t, i & 3);
+        return join(transposed(s.e + Tile::off(k, m)), transposed(s.e + Tile::off(k + 4, m)));
     }
     __device__ static Frag pack(const f32x4* t)
     {
@@ -101,6 +129,32 @@ template <> struct Mat<true> {
     __device__ static f32x4 mma(Frag a, Frag b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
     __device__ static El put(float v) { return (__bf16)v; }
     __device__ static float get(El v) { return (float)v; }
+};
+
+// An LDS tile of ROWS x COLS elements.  bf16: rows follow each other without
+// padding, so all would start in the same bank; the 16-byte pieces of a row lie
+// in an order that depends on the row (piece c at c xor swizzle(row)), such that
+// the 16 rows of rows() and the 4 rows x 4 pieces of a lane group in cols() lie
+// in different banks.  Float: rows 4 banks apart do that, at fixed distances from
+// one address a lane.
+template <typename El, int ROWS, int COLS> struct Tile {
+    static constexpr bool SWIZZLED = sizeof(El) == 2;
+    static constexpr int VE = 16 / sizeof(El), PIECES = COLS / VE, LD = SWIZZLED ? COLS : COLS + VE;
+    static_assert(!SWIZZLED || PIECES == 8 || PIECES == 16);
+    alignas(16) El e[ROWS * LD];
+
+    // (an operand's rows are 8 a + {0 .. 3} or 8 a + {4 .. 7}, a = 0 .. 3)
+    __device__ static constexpr int swizzle(int row)
+    {
+        return PIECES == 8 ? ((row >> 1) & 1) << 2 | ((row >> 3) & 3) : (row & 3) << 2 | ((row >> 3) & 3);
+    }
+    __device__ static constexpr int off(int row, int col)
+    {
+        if constexpr (SWIZZLED)
+            return row * LD + ((col / VE) ^ swizzle(row)) * VE + col % VE;
+        else
+            return row * LD + col;
+    }
 };
 
 // Storage types of the tensors
@@ -128,7 +182,7 @@ template <typename T> __device__ __forceinline__ const T* row_at(const T* p, int
 }
 
 // ROWS rows of `cols` elements from memory, `stride` bytes apart, on their way
-// into LDS rows of `ld` elements: load() issues every read at once (the values
+// into an LDS tile: load() issues every read at once (the values
 // wait in registers, so that reads of the next tile run while this one is
 // computed with), store() writes them, zeros in rows from `live` on and from
 // column `cols` to COLS.  Reads outside that range go to the last row or first
@@ -143,9 +197,9 @@ template <typename D, typename El, int COLS, int THREADS, bool VEC, int ROWS = 6
     static_assert(COLS % VE == 0 && THREADS % PER == 0 && ROWS % STEP == 0);
     u32x4 v[NL];
 
-    __device__ __forceinline__ void load(const T* src, uint32_t stride, int live, int cols, bool near)
+    __device__ __forceinline__ void load(const T* src, uint32_t stride, int live, int cols, bool near, int tid)
     {
-        const int r0 = threadIdx.x / PER, c = (threadIdx.x % PER) * VE;
+        const int r0 = tid / PER, c = (tid % PER) * VE;
         if constexpr (VEC) {
             const int c1 = c < cols ? c : 0;
             if (live >= ROWS && near) {
@@ -173,19 +227,19 @@ template <typename D, typename El, int COLS, int THREADS, bool VEC, int ROWS = 6
             }
         }
     }
-    __device__ __forceinline__ void store(El* lds, int ld, int live, int cols)
+    __device__ __forceinline__ void store(Tile<El, ROWS, COLS>& lds, int live, int cols, int tid)
     {
-        const int r0 = threadIdx.x / PER, c = (threadIdx.x % PER) * VE;
-        El* d = lds + r0 * ld + c;
+        const int r0 = tid / PER, c = (tid % PER) * VE;
         if (live >= ROWS && cols == COLS) {
 #pragma unroll
             for (int n = 0; n < NL; ++n)
-                *(u32x4*)(d + n * STEP * ld) = v[n];
+                *(u32x4*)(lds.e + lds.off(r0 + n * STEP, c)) = v[n];
         } else {
 #pragma unroll
             for (int n = 0; n < NL; ++n) {
                 const bool in = r0 + n * STEP < live && c < cols;
-                *(u32x4*)(d + n * STEP * ld) = u32x4{in ? v[n].x : 0, in ? v[n].y : 0, in ? v[n].z : 0, in ? v[n].w : 0};
+                *(u32x4*)(lds.e + lds.off(r0 + n * STEP, c)) =
+                    u32x4{in ? v[n].x : 0, in ? v[n].y : 0, in ? v[n].z : 0, in ? v[n].w : 0};
             }
         }
     }
@@ -198,9 +252,9 @@ template <typename El, int ROWS, int COLS, int THREADS> struct Dense {
     static_assert(THREADS % PER == 0 && ROWS % STEP == 0);
     u32x4 v[NL];
 
-    __device__ __forceinline__ void load(const El* src, int live = ROWS)
+    __device__ __forceinline__ void load(const El* src, int live, int tid)
     {
-        const int r0 = threadIdx.x / PER, c = (threadIdx.x % PER) * VE;
+        const int r0 = tid / PER, c = (tid % PER) * VE;
         if (live >= ROWS) {
             const uint32_t off = (uint32_t)(r0 * COLS + c) * (uint32_t)sizeof(El);
 #pragma unroll
@@ -212,69 +266,69 @@ template <typename El, int ROWS, int COLS, int THREADS> struct Dense {
                 v[n] = *(const u32x4*)(src + min(r0 + n * STEP, live - 1) * COLS + c);
         }
     }
-    __device__ __forceinline__ void store(El* lds, int ld, int live = ROWS)
+    __device__ __forceinline__ void store(Tile<El, ROWS, COLS>& lds, int live, int tid)
     {
-        const int r0 = threadIdx.x / PER, c = (threadIdx.x % PER) * VE;
-        El* d = lds + r0 * ld + c;
+        const int r0 = tid / PER, c = (tid % PER) * VE;
         if (live >= ROWS) {
 #pragma unroll
             for (int n = 0; n < NL; ++n)
-                *(u32x4*)(d + n * STEP * ld) = v[n];
+                *(u32x4*)(lds.e + lds.off(r0 + n * STEP, c)) = v[n];
         } else {
 #pragma unroll
             for (int n = 0; n < NL; ++n) {
                 const bool in = r0 + n * STEP < live;
-                *(u32x4*)(d + n * STEP * ld) = u32x4{in ? v[n].x : 0, in ? v[n].y : 0, in ? v[n].z : 0, in ? v[n].w : 0};
+                *(u32x4*)(lds.e + lds.off(r0 + n * STEP, c)) =
+                    u32x4{in ? v[n].x : 0, in ? v[n].y : 0, in ? v[n].z : 0, in ? v[n].w : 0};
             }
         }
     }
 };
 
-// A column's values at the steps of four result tiles (row 16 t + 4 g + r in
+// A column's values at the steps of four result tiles (step M::at(t, g) + r in
 // [t][r]); steps from `live` on give the last one's, whatever it holds
-template <typename T> struct Column {
+template <typename M, typename T> struct Column {
     T x[4][4];
 
-    __device__ __forceinline__ void load(const T* src, int v, uint32_t stride, int live, bool near)
+    __device__ __forceinline__ void load(const T* src, int v, uint32_t stride, int live, bool near, int tid)
     {
-        const int g4 = 4 * ((threadIdx.x & 63) >> 4);
+        const int g = (tid & 63) >> 4;
         if (live >= 64 && near) {
-            const uint32_t off = (uint32_t)g4 * stride + (uint32_t)v * (uint32_t)sizeof(T);
+            const uint32_t off = (uint32_t)M::at(0, g) * stride + (uint32_t)v * (uint32_t)sizeof(T);
 #pragma unroll
             for (int t = 0; t < 4; ++t)
 #pragma unroll
                 for (int r = 0; r < 4; ++r)
-                    x[t][r] = *(const T*)((const char*)src + (uint64_t)(16 * t + r) * stride + off);
+                    x[t][r] = *(const T*)((const char*)src + (uint64_t)(M::at(t, 0) + r) * stride + off);
         } else {
 #pragma unroll
             for (int t = 0; t < 4; ++t)
 #pragma unroll
                 for (int r = 0; r < 4; ++r)
-                    x[t][r] = *row_at(src + v, min(16 * t + g4 + r, live - 1), stride);
+                    x[t][r] = *row_at(src + v, min(M::at(t, g) + r, live - 1), stride);
         }
     }
 };
 
 // The reverse: steps below `live` are written
-template <typename D>
-__device__ __forceinline__ void store_column(const f32x4* x, typename D::T* dst, int v, uint32_t stride, int live, bool near)
+template <typename M, typename D>
+__device__ __forceinline__ void store_column(const f32x4* x, typename D::T* dst, int v, uint32_t stride, int live, bool near, int tid)
 {
     using T = typename D::T;
-    const int g4 = 4 * ((threadIdx.x & 63) >> 4);
+    const int g = (tid & 63) >> 4;
     if (live >= 64 && near) {
-        const uint32_t off = (uint32_t)g4 * stride + (uint32_t)v * (uint32_t)sizeof(T);
+        const uint32_t off = (uint32_t)M::at(0, g) * stride + (uint32_t)v * (uint32_t)sizeof(T);
 #pragma unroll
         for (int t = 0; t < 4; ++t)
 #pragma unroll
             for (int r = 0; r < 4; ++r)
-                *(T*)((char*)dst + (uint64_t)(16 * t + r) * stride + off) = D::put(x[t][r]);
+                *(T*)((char*)dst + (uint64_t)(M::at(t, 0) + r) * stride + off) = D::put(x[t][r]);
     } else {
 #pragma unroll
         for (int t = 0; t < 4; ++t)
 #pragma unroll
             for (int r = 0; r < 4; ++r)
-                if (16 * t + g4 + r < live)
-                    *const_cast<T*>(row_at(dst + v, 16 * t + g4 + r, stride)) = D::put(x[t][r]);
+                if (M::at(t, g) + r < live)
+                    *const_cast<T*>(row_at(dst + v, M::at(t, g) + r, stride)) = D::put(x[t][r]);
     }
 }
 
