@@ -283,6 +283,8 @@ int mfpsn_delta_forward(const mfpsn_delta_desc* desc, const void* q, const void*
     a.state_in = state_in;
     a.o = o;
     a.state_out = state_out;
+    const int es = elem_bytes(desc->dtype);
+    a.vec_v = wide_rows(v, a.v_row, desc->Dv, es) && wide_rows(o, (int64_t)desc->Hv * desc->Dv, desc->Dv, es);
     if (!steps)
         place(a, l, saved ? saved : workspace, saved != nullptr);
     const hipStream_t s = (hipStream_t)stream;

@@ -21,7 +21,7 @@ struct DeltaArgs {
     int64_t q_row, k_row, v_row;  // elements between the rows of consecutive (t, n)
     uint32_t q_step, k_step, v_step, o_step, g_step;  // bytes between consecutive t (o: grad_o and grad_v too)
     int32_t near;                 // 64 of the longest of these steps fit 32 bits
-    int32_t vec_qk, vec_v;        // rows of q and k (of the gradients) may be read and written 16 bytes at a time
+    int32_t vec_qk, vec_v;        // rows of q and k (of v and o, of the gradients) may be accessed 16 bytes at a time
     int32_t nc;                   // chunks of the longest sequence
     int32_t dvp;                  // Dv rounded up to 16
     const void *q, *k, *v, *g, *beta;

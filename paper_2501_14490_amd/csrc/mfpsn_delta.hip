@@ -257,6 +257,8 @@ template <bool BF, int DKP> struct ScanLds {
     using El = typename Mat<BF>::El;
     Tile<El, L, DKP> k, q;
     Tile<El, L, L> x[BF ? 2 : 1], p;
+    Tile<El, L, 64> v;  // [i][v]
+    Tile<El, 64, L> o;  // [v][i]
     alignas(16) float gate[3 * L];
 };
 
@@ -269,15 +271,15 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(1, 1)))
     using Frag = typename M::Frag;
     using Lds = ScanLds<BF, DKP>;
     constexpr int TK = DKP / 16, TH = NW * 64, KU = M::KU, TU = M::TU, UK = DKP / KU, UL = L / KU;
-    static_assert(TH >= 3 * L);
+    static_assert(NW == 4 && TH >= 3 * L);
     __shared__ Lds s;
     const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, col = lane & 15, g = lane >> 4;
     const int vblocks = (a.dvp + 16 * NW - 1) / (16 * NW);
     const int64_t head = blockIdx.x / vblocks;
     const int n = (int)(head / a.Hv), hv = (int)(head - (int64_t)n * a.Hv), hk = hv / (a.Hv / a.Hk);
-    const int v = ((int)(blockIdx.x % vblocks) * NW + wave) * 16 + col;
+    const int v0 = (int)(blockIdx.x % vblocks) * 64, vl = M::at(wave, col >> 2) + (col & 3), v = v0 + vl, cols = min(64, a.Dv - v0);
     const bool mine = v < a.Dv;         // a column of the tensors
-    const bool wide = v - col < a.dvp;  // the wave has columns of the padded arrays
+    const bool wide = v < a.dvp;        // a column of the padded arrays
     const int len = length_of(a, n), chunks = (len + L - 1) / L;
     f32x4 S[TK];
 #pragma unroll
@@ -288,23 +290,32 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(1, 1)))
             S[t][r] = a.state_in && mine && d < a.Dk ? a.state_in[(head * a.Dk + d) * a.Dv + v] : 0.0f;
         }
     Rows<D, El, DKP, TH, VEC> nk, nq;
+    Rows<D, El, 64, TH, VEC> nv;
     Dense<El, L, L, TH> nx[BF ? 2 : 1], np;
-    Column<M, T> nv;
     float ngate;
-    const auto fetch = [&](int c, int tid) {
+    // The chunk's tiles in four parts (a wave waits where it issues more reads than the memory pipe takes)
+    const auto fetch = [&](int c, int part, int tid) {
         const int t0 = c * L, live = min(L, len - t0);
         const int64_t row0 = (int64_t)t0 * a.N + n, unit = unit_of(a, n, hv, c);
-        nk.load((const T*)a.k + row0 * a.k_row + (int64_t)hk * a.Dk, a.k_step, live, a.Dk, a.near, tid);
-        nq.load((const T*)a.q + row0 * a.q_row + (int64_t)hk * a.Dk, a.q_step, live, a.Dk, a.near, tid);
-        nx[0].load((const El*)a.X + unit * L * L * (BF ? 2 : 1), L, tid);
-        if constexpr (BF)
-            nx[1].load((const El*)a.X + unit * L * L * 2 + L * L, L, tid);
-        np.load((const El*)a.P + unit * L * L, L, tid);
-        nv.load((const T*)a.v + row0 * a.v_row + (int64_t)hv * a.Dv, mine ? v : 0, a.v_step, live, a.near, tid);
-        ngate = a.gate[unit * 3 * L + min(tid, 3 * L - 1)];
+        if (part == 0)
+            nk.load((const T*)a.k + row0 * a.k_row + (int64_t)hk * a.Dk, a.k_step, live, a.Dk, a.near, tid);
+        if (part == 1)
+            nq.load((const T*)a.q + row0 * a.q_row + (int64_t)hk * a.Dk, a.q_step, live, a.Dk, a.near, tid);
+        if (part == 2) {
+            nx[0].load((const El*)a.X + unit * L * L * (BF ? 2 : 1), L, tid);
+            if constexpr (BF)
+                nx[1].load((const El*)a.X + unit * L * L * 2 + L * L, L, tid);
+        }
+        if (part == 3) {
+            np.load((const El*)a.P + unit * L * L, L, tid);
+            nv.load((const T*)a.v + row0 * a.v_row + (int64_t)hv * a.Dv + v0, a.v_step, live, cols, a.near, tid);
+            ngate = a.gate[unit * 3 * L + min(tid, 3 * L - 1)];
+        }
     };
     if (chunks > 0)
-        fetch(0, tid);
+#pragma unroll
+        for (int part = 0; part < 4; ++part)
+            fetch(0, part, tid);
     for (int c = 0; c < chunks; ++c) {
         const int t0 = c * L, live = min(L, len - t0);
         const int64_t row0 = (int64_t)t0 * a.N + n, unit = unit_of(a, n, hv, c);
@@ -317,20 +328,11 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(1, 1)))
         np.store(s.p, L, tid);
         if (tid < 3 * L)
             s.gate[tid] = ngate;
-        f32x4 R[4];
-#pragma unroll
-        for (int t = 0; t < 4; ++t)
-            R[t] = f32x4{D::get(nv.x[t][0]), D::get(nv.x[t][1]), D::get(nv.x[t][2]), D::get(nv.x[t][3])};
-        if (live < L || !mine) {
-#pragma unroll
-            for (int t = 0; t < 4; ++t)
-#pragma unroll
-                for (int r = 0; r < 4; ++r)
-                    R[t][r] = mine && M::at(t, g) + r < live ? R[t][r] : 0.0f;
-        }
+        nv.store(s.v, live, cols, tid);
+        if (c > 0)  // the chunk before, whose outputs wait in LDS
+            store_rows<M, D, VEC>(s.o, (T*)a.o + ((row0 - (int64_t)L * a.N) * a.Hv + hv) * a.Dv + v0, a.o_step, L, cols,
+                                  again(threadIdx.x));
         __syncthreads();
-        if (c + 1 < chunks)
-            fetch(c + 1, again(threadIdx.x));
         if (a.S0 && wide) {  // [v][d], for the backward
             El* S0 = (El*)a.S0 + (unit * a.dvp + v) * DKP + M::at(0, g);
 #pragma unroll
@@ -338,8 +340,8 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(1, 1)))
                 *(Frag*)(S0 + u * KU) = M::pack(S + u * TU);
         }
         // K S0 and Q S0.  16-bit: the state goes in as the sum of two numbers of 8 bits each.
-        f32x4 KS[4], O[4], eG[4], sG[4], gam[4];
-        Frag fk[2][4], fq[2][4], fx[UL][4], fl[UL][4], fp[UL][4], ft[2][TK];
+        f32x4 R[4], KS[4], O[4], eG[4], sG[4], gam[4];
+        Frag fv[UL], fk[2][4], fq[2][4], fx[UL][4], fl[UL][4], fp[UL][4], ft[2][TK];
         const auto read_kq = [&](int u) {
 #pragma unroll
             for (int t = 0; t < 4; ++t) {
@@ -354,6 +356,11 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(1, 1)))
         in_order();
 #pragma unroll
         for (int u = 0; u < UK; ++u) {
+            if (c + 1 < chunks)
+#pragma unroll
+                for (int part = 0; part < 4; ++part)
+                    if (part * UK / 4 == u)
+                        fetch(c + 1, part, again(threadIdx.x));
             if (u + 1 < UK) {
                 read_kq(u + 1);
             } else {
@@ -391,11 +398,13 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(1, 1)))
             in_order();
         }
 #pragma unroll
-        for (int w = 0; w < UL; ++w)
+        for (int w = 0; w < UL; ++w) {
+            fv[w] = M::cols(s.v, wave, w, tid);
 #pragma unroll
             for (int t = 0; t < 4; ++t)
                 if (M::reaches(w * TU, t))
                     fp[w][t] = M::rows(s.p, t, w, tid);
+        }
         in_order();
         // residuals r = X (V - diag(e^G) K S0)
         f32x4 U[4];
@@ -404,7 +413,7 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(1, 1)))
             U[t] = f32x4{0, 0, 0, 0};
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                R[t][r] = __builtin_fmaf(-eG[t][r], KS[t][r], R[t][r]);
+                R[t][r] = __builtin_fmaf(-eG[t][r], KS[t][r], M::get(fv[t / TU][4 * (t % TU) + r]));
                 O[t][r] *= sG[t][r];
             }
         }
@@ -483,8 +492,14 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(1, 1)))
             }
             in_order();
         }
-        if (mine)
-            store_column<M, D>(O, (T*)a.o + (row0 * a.Hv + hv) * a.Dv, v, a.o_step, live, a.near, again(threadIdx.x));
+#pragma unroll
+        for (int u = 0; u < UL; ++u)
+            *(Frag*)(s.o.e + s.o.off(vl, u * KU + M::at(0, g))) = M::pack(O + u * TU);
+    }
+    if (chunks > 0) {  // the last chunk's outputs
+        __syncthreads();
+        const int64_t row0 = (int64_t)(chunks - 1) * L * a.N + n;
+        store_rows<M, D, VEC>(s.o, (T*)a.o + (row0 * a.Hv + hv) * a.Dv + v0, a.o_step, len - (chunks - 1) * L, cols, tid);
     }
     if (!mine)
         return;
@@ -507,6 +522,8 @@ template <bool BF, int DKP> struct RscanLds {
     using El = typename Mat<BF>::El;
     Tile<El, L, DKP> k, q;
     Tile<El, L, L> x, p;
+    Tile<El, L, 64> dO;  // [i][v]
+    Tile<El, 64, L> dV;  // [v][i]
     alignas(16) float gate[3 * L];
 };
 
@@ -519,14 +536,14 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(1, 1)))
     using Frag = typename M::Frag;
     using Lds = RscanLds<BF, DKP>;
     constexpr int TK = DKP / 16, TH = NW * 64, KU = M::KU, TU = M::TU, UK = DKP / KU, UL = L / KU;
-    static_assert(TH >= 3 * L);
+    static_assert(NW == 4 && TH >= 3 * L);
     __shared__ Lds s;
     const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, col = lane & 15, g = lane >> 4;
     const int vblocks = (a.dvp + 16 * NW - 1) / (16 * NW);
     const int64_t head = blockIdx.x / vblocks;
     const int n = (int)(head / a.Hv), hv = (int)(head - (int64_t)n * a.Hv), hk = hv / (a.Hv / a.Hk);
-    const int v = ((int)(blockIdx.x % vblocks) * NW + wave) * 16 + col;
-    const bool mine = v < a.Dv, wide = v - col < a.dvp;
+    const int v0 = (int)(blockIdx.x % vblocks) * 64, vl = M::at(wave, col >> 2) + (col & 3), v = v0 + vl, cols = min(64, a.Dv - v0);
+    const bool mine = v < a.Dv, wide = v < a.dvp;
     const int len = length_of(a, n), chunks = (len + L - 1) / L;
     f32x4 S[TK];
 #pragma unroll
@@ -537,21 +554,29 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(1, 1)))
             S[t][r] = a.grad_state_out && mine && d < a.Dk ? a.grad_state_out[(head * a.Dk + d) * a.Dv + v] : 0.0f;
         }
     Rows<D, El, DKP, TH, VEC> nk, nq;
+    Rows<D, El, 64, TH, VEC> no;
     Dense<El, L, L, TH> nx, np;
-    Column<M, T> no;
     float ngate;
-    const auto fetch = [&](int c, int tid) {
+    const auto fetch = [&](int c, int part, int tid) {
         const int t0 = c * L, live = min(L, len - t0);
         const int64_t row0 = (int64_t)t0 * a.N + n, unit = unit_of(a, n, hv, c);
-        nk.load((const T*)a.k + row0 * a.k_row + (int64_t)hk * a.Dk, a.k_step, live, a.Dk, a.near, tid);
-        nq.load((const T*)a.q + row0 * a.q_row + (int64_t)hk * a.Dk, a.q_step, live, a.Dk, a.near, tid);
-        nx.load((const El*)a.X + unit * L * L * (BF ? 2 : 1), L, tid);
-        np.load((const El*)a.P + unit * L * L, L, tid);
-        no.load((const T*)a.grad_o + (row0 * a.Hv + hv) * a.Dv, mine ? v : 0, a.o_step, live, a.near, tid);
-        ngate = a.gate[unit * 3 * L + min(tid, 3 * L - 1)];
+        if (part == 0)
+            nk.load((const T*)a.k + row0 * a.k_row + (int64_t)hk * a.Dk, a.k_step, live, a.Dk, a.near, tid);
+        if (part == 1)
+            nq.load((const T*)a.q + row0 * a.q_row + (int64_t)hk * a.Dk, a.q_step, live, a.Dk, a.near, tid);
+        if (part == 2) {
+            nx.load((const El*)a.X + unit * L * L * (BF ? 2 : 1), L, tid);
+            np.load((const El*)a.P + unit * L * L, L, tid);
+        }
+        if (part == 3) {
+            no.load((const T*)a.grad_o + (row0 * a.Hv + hv) * a.Dv + v0, a.o_step, live, cols, a.near, tid);
+            ngate = a.gate[unit * 3 * L + min(tid, 3 * L - 1)];
+        }
     };
     if (chunks > 0)
-        fetch(chunks - 1, tid);
+#pragma unroll
+        for (int part = 0; part < 4; ++part)
+            fetch(chunks - 1, part, tid);
     for (int c = chunks - 1; c >= 0; --c) {
         const int t0 = c * L, live = min(L, len - t0);
         const int64_t row0 = (int64_t)t0 * a.N + n, unit = unit_of(a, n, hv, c);
@@ -562,20 +587,11 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(1, 1)))
         np.store(s.p, L, tid);
         if (tid < 3 * L)
             s.gate[tid] = ngate;
-        f32x4 dO[4];
-#pragma unroll
-        for (int t = 0; t < 4; ++t)
-            dO[t] = f32x4{D::get(no.x[t][0]), D::get(no.x[t][1]), D::get(no.x[t][2]), D::get(no.x[t][3])};
-        if (live < L || !mine) {
-#pragma unroll
-            for (int t = 0; t < 4; ++t)
-#pragma unroll
-                for (int r = 0; r < 4; ++r)
-                    dO[t][r] = mine && M::at(t, g) + r < live ? dO[t][r] : 0.0f;
-        }
+        no.store(s.dO, live, cols, tid);
+        if (c + 1 < chunks)  // the chunk behind, whose gradients wait in LDS
+            store_rows<M, D, VEC>(s.dV, (T*)a.grad_v + ((row0 + (int64_t)L * a.N) * a.Hv + hv) * a.Dv + v0, a.o_step,
+                                  min(L, len - t0 - L), cols, again(threadIdx.x));
         __syncthreads();
-        if (c > 0)
-            fetch(c - 1, again(threadIdx.x));
         if (wide) {  // [v][d], for delta_grads
             El* dS = (El*)a.dS + (unit * a.dvp + v) * DKP + M::at(0, g);
 #pragma unroll
@@ -583,8 +599,8 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(1, 1)))
                 *(Frag*)(dS + u * KU) = M::pack(S + u * TU);
         }
         // dr' = diag(e^{G_last - G} beta) K dS1 + P^T dO
-        f32x4 R[4], eG[4], sG[4], gam[4];
-        Frag fk[2][4], fp[UL][4], fx[UL][4], ft[2][TK];
+        f32x4 R[4], dO[4], eG[4], sG[4], gam[4];
+        Frag fo[UL], fk[2][4], fp[UL][4], fx[UL][4], ft[2][TK];
         const auto read_k = [&](int u) {
 #pragma unroll
             for (int t = 0; t < 4; ++t)
@@ -597,9 +613,17 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(1, 1)))
         in_order();
 #pragma unroll
         for (int u = 0; u < UK; ++u) {
+            if (c > 0)
+#pragma unroll
+                for (int part = 0; part < 4; ++part)
+                    if (part * UK / 4 == u)
+                        fetch(c - 1, part, again(threadIdx.x));
             if (u + 1 < UK) {
                 read_k(u + 1);
             } else {
+#pragma unroll
+                for (int w = 0; w < UL; ++w)
+                    fo[w] = M::cols(s.dO, wave, w, tid);
 #pragma unroll
                 for (int t = 0; t < 4; ++t) {
                     eG[t] = *(const f32x4*)(s.gate + M::at(t, g));
@@ -640,11 +664,10 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(1, 1)))
                 R[t][r] *= gam[t][r];
 #pragma unroll
         for (int u = 0; u < UL; ++u) {
-            const Frag b = M::pack(dO + u * TU);
 #pragma unroll
             for (int t = 0; t < 4; ++t)
                 if (M::reaches(t, u * TU))
-                    R[t] = M::mma(fp[u][t], b, R[t]);
+                    R[t] = M::mma(fp[u][t], fo[u], R[t]);
         }
         // dV = X^T dr', and meanwhile dS0 = e^{G_last} dS1 + scale Q^T diag(e^G) dO - K^T diag(e^G) dV
         f32x4 dV[4];
@@ -654,7 +677,7 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(1, 1)))
             dV[t] = f32x4{0, 0, 0, 0};
 #pragma unroll
             for (int r = 0; r < 4; ++r)
-                dO[t][r] *= sG[t][r];
+                dO[t][r] = sG[t][r] * M::get(fo[t / TU][4 * (t % TU) + r]);
         }
 #pragma unroll
         for (int t = 0; t < TK; ++t)
@@ -682,8 +705,9 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(1, 1)))
                 if (M::reaches(t, u * TU))
                     dV[t] = M::mma(fx[u][t], b, dV[t]);
         }
-        if (mine)
-            store_column<M, D>(dV, (T*)a.grad_v + (row0 * a.Hv + hv) * a.Dv, v, a.o_step, live, a.near, again(threadIdx.x));
+#pragma unroll
+        for (int u = 0; u < UL; ++u)
+            *(Frag*)(s.dV.e + s.dV.off(vl, u * KU + M::at(0, g))) = M::pack(dV + u * TU);
 #pragma unroll
         for (int t = 0; t < 4; ++t)
 #pragma unroll
@@ -700,6 +724,10 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(1, 1)))
                 S[t] = M::mma(ft[u & 1][t], b, S[t]);
             in_order();
         }
+    }
+    if (chunks > 0) {  // the first chunk's gradients
+        __syncthreads();
+        store_rows<M, D, VEC>(s.dV, (T*)a.grad_v + ((int64_t)n * a.Hv + hv) * a.Dv + v0, a.o_step, min(L, len), cols, tid);
     }
     if (!mine)
         return;
@@ -1073,7 +1101,7 @@ template <bool VEC> hipError_t run(const DeltaArgs& a, int dtype, bool bwd, hipS
 
 hipError_t launch_delta_forward(const DeltaArgs& a, int dtype, hipStream_t s)
 {
-    return a.vec_qk ? run<true>(a, dtype, false, s) : run<false>(a, dtype, false, s);
+    return a.vec_qk && a.vec_v ? run<true>(a, dtype, false, s) : run<false>(a, dtype, false, s);
 }
 
 hipError_t launch_delta_backward(const DeltaArgs& a, int dtype, hipStream_t s)

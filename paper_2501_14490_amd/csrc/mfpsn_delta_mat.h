@@ -284,51 +284,30 @@ template <typename El, int ROWS, int COLS, int THREADS> struct Dense {
     }
 };
 
-// A column's values at the steps of four result tiles (step M::at(t, g) + r in
-// [t][r]); steps from `live` on give the last one's, whatever it holds
-template <typename M, typename T> struct Column {
-    T x[4][4];
-
-    __device__ __forceinline__ void load(const T* src, int v, uint32_t stride, int live, bool near, int tid)
-    {
-        const int g = (tid & 63) >> 4;
-        if (live >= 64 && near) {
-            const uint32_t off = (uint32_t)M::at(0, g) * stride + (uint32_t)v * (uint32_t)sizeof(T);
-#pragma unroll
-            for (int t = 0; t < 4; ++t)
-#pragma unroll
-                for (int r = 0; r < 4; ++r)
-                    x[t][r] = *(const T*)((const char*)src + (uint64_t)(M::at(t, 0) + r) * stride + off);
-        } else {
-#pragma unroll
-            for (int t = 0; t < 4; ++t)
-#pragma unroll
-                for (int r = 0; r < 4; ++r)
-                    x[t][r] = *row_at(src + v, min(M::at(t, g) + r, live - 1), stride);
-        }
-    }
-};
-
-// The reverse: steps below `live` are written
-template <typename M, typename D>
-__device__ __forceinline__ void store_column(const f32x4* x, typename D::T* dst, int v, uint32_t stride, int live, bool near, int tid)
+// 64 steps' values of 64 columns from an LDS tile [column][step], 16 bytes at a
+// time, by four waves (wave w: row tile w of the steps): steps below `live`,
+// columns below `cols`.  VEC: as above, also of dst.
+template <typename M, typename D, bool VEC>
+__device__ __forceinline__ void store_rows(const Tile<typename M::El, 64, 64>& lds, typename D::T* dst, uint32_t stride,
+                                           int live, int cols, int tid)
 {
     using T = typename D::T;
-    const int g = (tid & 63) >> 4;
-    if (live >= 64 && near) {
-        const uint32_t off = (uint32_t)M::at(0, g) * stride + (uint32_t)v * (uint32_t)sizeof(T);
+    constexpr int VE = 16 / sizeof(T);
+    const int wave = tid >> 6, col = tid & 15, g = (tid & 63) >> 4, i = M::at(wave, col >> 2) + (col & 3);
+    T* row = const_cast<T*>(row_at(dst, i, stride));
 #pragma unroll
-        for (int t = 0; t < 4; ++t)
+    for (int u = 0; u < 64 / M::KU; ++u) {
+        const typename M::Frag f = M::cols(lds, wave, u, tid);
+        const int v = u * M::KU + M::at(0, g);
+        if constexpr (VEC) {
+            if (i < live && v < cols)
+                *(typename M::Frag*)(row + v) = f;
+        } else if (i < live) {
 #pragma unroll
-            for (int r = 0; r < 4; ++r)
-                *(T*)((char*)dst + (uint64_t)(M::at(t, 0) + r) * stride + off) = D::put(x[t][r]);
-    } else {
-#pragma unroll
-        for (int t = 0; t < 4; ++t)
-#pragma unroll
-            for (int r = 0; r < 4; ++r)
-                if (M::at(t, g) + r < live)
-                    *const_cast<T*>(row_at(dst + v, M::at(t, g) + r, stride)) = D::put(x[t][r]);
+            for (int j = 0; j < VE; ++j)
+                if (v + j < cols)
+                    row[v + j] = f[j];
+        }
     }
 }
 
