@@ -24,19 +24,15 @@ struct NormArgs {
     float* grad_beta;    // nullable
 };
 
-// Upper bound of the backward's blocks, and so of its partial rows: the
-// partial sums of 2 C floats a block stay below 1/8 of the bytes that the
-// block's share of x and grad_y has (see norm_blocks), and 1024 blocks of 4
-// waves are 4 waves for each SIMD.
-constexpr int kNormMaxBlocks = 1024;
-
 // Blocks of the backward for M rows of C channels and S columns (host; the
-// workspace is sized by it)
+// workspace has 2 C floats for each): one for 4 rows (S = 1) or a tile of 64
+// columns, up to 4 waves for each SIMD, 8 for few channels, whose tiles are
+// short of loads in flight and whose partial sums are small.
+constexpr int kNormMaxBlocks = 2048;
 inline int norm_blocks(int64_t M, int64_t C, int64_t S)
 {
-    (void)C;
-    const int64_t work = (M * S + 15) / 16;  // 16 columns for a block at least
-    return (int)(work < 1 ? 1 : (work < kNormMaxBlocks ? work : kNormMaxBlocks));
+    const int64_t work = S == 1 ? (M + 3) / 4 : (M * S + 63) / 64, most = C <= 256 ? kNormMaxBlocks : kNormMaxBlocks / 2;
+    return (int)(work < 1 ? 1 : (work < most ? work : most));
 }
 
 hipError_t launch_norm_forward(const NormArgs& a, int dtype, hipStream_t stream);

@@ -10,7 +10,9 @@
 //
 // Both passes are HBM-bound (one read of each input, one write of each output;
 // about 10 flops an element).  A row's values are loaded once and stay in
-// registers between its statistics and its outputs, so the variance can be
+// registers between its statistics and its outputs (all of its reads are
+// issued before the first is used; those behind a row's end read its beginning,
+// since a read under a condition is waited for by itself), so the variance can be
 // the mean of the squared deviations (two passes over registers) instead of a
 // difference of two large sums.  All sums are float; ggamma and gbeta are
 // summed by each thread over the columns of its block, then over a block's
@@ -49,6 +51,26 @@ template <typename T, int N> struct alignas(sizeof(T) * N) Vec {
     T v[N];
 };
 
+// The same value, not known to be: what is computed from it is computed anew
+// (known as one, the planes' addresses and the floats of all their 16-bit values
+// are kept over a tile, twice the registers)
+__device__ __forceinline__ int again(int v)
+{
+    asm volatile("" : "+v"(v));
+    return v;
+}
+template <typename V> __device__ __forceinline__ void again(V& v)
+{
+    if constexpr (sizeof(V) % 4 == 0) {
+        uint32_t w[sizeof(V) / 4];
+        __builtin_memcpy(w, &v, sizeof(V));
+#pragma unroll
+        for (uint32_t& x : w)
+            asm volatile("" : "+v"(x));
+        __builtin_memcpy(&v, w, sizeof(V));
+    }
+}
+
 __device__ __forceinline__ float wave_sum(float v)
 {
 #pragma unroll
@@ -77,6 +99,26 @@ __device__ __forceinline__ float row_sum(float v, float (*lds)[4], int& at)
     return v;
 }
 
+// A thread's weights w[at0 + i step + j] (behind C: any), `none` where there are none
+template <int VE, int NV>
+__device__ __forceinline__ void load_weights(const float* __restrict__ w, float none, int at0, int step, int C,
+                                             float (&out)[NV][VE])
+{
+    if (w) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+            for (int j = 0; j < VE; ++j)
+                out[i][j] = w[min(at0 + i * step + j, C - 1)];
+    } else {
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+            for (int j = 0; j < VE; ++j)
+                out[i][j] = none;
+    }
+}
+
 // ---------------------------------------------------------------------------
 // S = 1
 // ---------------------------------------------------------------------------
@@ -93,21 +135,27 @@ __global__ __launch_bounds__(kT) void norm_fwd_rows(NormArgs a)
     const int lane = threadIdx.x % LANES, sub = threadIdx.x / LANES;
     const int C = a.C;
     const float inv = 1.0f / (float)C;
+    float gam[NV][VE], bet[NV][VE];
+    load_weights<VE, NV>(a.gamma, 1.0f, lane * VE, LANES * VE, C, gam);
+    load_weights<VE, NV>(a.beta, 0.0f, lane * VE, LANES * VE, C, bet);
     for (int64_t m = (int64_t)blockIdx.x * ROWS + sub; m < a.M; m += (int64_t)gridDim.x * ROWS) {
         const T* __restrict__ x = (const T*)a.x + m * C;
         T* __restrict__ y = (T*)a.out + m * C;
+        V raw[NV];
         float f[NV][VE];
         float s = 0.0f;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int e = (i * LANES + lane) * VE;
-            V v = {};
-            if (e < C)
-                v = *(const V*)(x + e);
+            raw[i] = *(const V*)(x + (e < C ? e : 0));
+        }
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int e = (i * LANES + lane) * VE;
 #pragma unroll
             for (int j = 0; j < VE; ++j) {
-                f[i][j] = D::get(v.v[j]);
-                s += f[i][j];
+                f[i][j] = D::get(raw[i].v[j]);
+                s += e < C ? f[i][j] : 0.0f;
             }
         }
         const float mean = row_sum<WPR>(s, lds, at) * inv;
@@ -133,7 +181,7 @@ __global__ __launch_bounds__(kT) void norm_fwd_rows(NormArgs a)
                 V v;
 #pragma unroll
                 for (int j = 0; j < VE; ++j)
-                    v.v[j] = D::put(f[i][j] * rstd * (a.gamma ? a.gamma[e + j] : 1.0f) + (a.beta ? a.beta[e + j] : 0.0f));
+                    v.v[j] = D::put(f[i][j] * rstd * gam[i][j] + bet[i][j]);
                 *(V*)(y + e) = v;
             }
         }
@@ -183,34 +231,27 @@ __global__ __launch_bounds__(kT) void norm_bwd_rows(NormArgs a)
     const int C = a.C;
     const float inv = 1.0f / (float)C;
     float gg[NV][VE] = {}, gb[NV][VE] = {}, gam[NV][VE];
-#pragma unroll
-    for (int i = 0; i < NV; ++i)
-#pragma unroll
-        for (int j = 0; j < VE; ++j) {
-            const int e = (i * LANES + lane) * VE + j;
-            gam[i][j] = e < C ? (a.gamma ? a.gamma[e] : 1.0f) : 0.0f;
-        }
+    load_weights<VE, NV>(a.gamma, 1.0f, lane * VE, LANES * VE, C, gam);
     for (int64_t m = (int64_t)blockIdx.x * ROWS + sub; m < a.M; m += (int64_t)gridDim.x * ROWS) {
         const T* __restrict__ x = (const T*)a.x + m * C;
         const T* __restrict__ gy = (const T*)a.gy + m * C;
         T* __restrict__ gx = (T*)a.out + m * C;
         const float mean = a.mean[m], rstd = a.rstd[m];
-        V vx[NV] = {}, vg[NV] = {};
+        V vx[NV], vg[NV];
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const int e = (i * LANES + lane) * VE;
-            if (e < C) {
-                vx[i] = *(const V*)(x + e);
-                vg[i] = *(const V*)(gy + e);
-            }
+            const int e = (i * LANES + lane) * VE, at = e < C ? e : 0;
+            vx[i] = *(const V*)(x + at);
+            vg[i] = *(const V*)(gy + at);
         }
         float sa = 0.0f, sh = 0.0f;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
+            const bool in = (i * LANES + lane) * VE < C;
 #pragma unroll
             for (int j = 0; j < VE; ++j) {
-                const float g = D::get(vg[i].v[j]), xh = (D::get(vx[i].v[j]) - mean) * rstd;
-                gg[i][j] += g * xh;  // (lanes behind the row: g = 0)
+                const float g = in ? D::get(vg[i].v[j]) : 0.0f, xh = in ? (D::get(vx[i].v[j]) - mean) * rstd : 0.0f;
+                gg[i][j] += g * xh;
                 gb[i][j] += g;
                 const float al = g * gam[i][j];
                 sa += al;
@@ -319,9 +360,17 @@ template <int VE, int LX, int NW> struct Plane {
     static constexpr int LY = 64 / LX, W = LX * VE, STEP = NW * LY, THREADS = NW * 64;
 };
 
+// The block's first tile: the blocks of one XCD (every eighth) take neighbouring
+// tiles, so that cache lines that two tiles share are fetched into one L2
+__device__ __forceinline__ int64_t first_tile()
+{
+    const uint32_t b = blockIdx.x, n = gridDim.x;
+    return n % 8 == 0 ? (b % 8) * (n / 8) + b / 8 : b;
+}
+
 // Sums over the channels of VE columns: over the lanes' rows, then the waves
 template <int VE, int LX, int NW>
-__device__ __forceinline__ void column_sum(float (&v)[VE], float (*lds)[NW][LX * VE])
+__device__ __forceinline__ void column_sum(float (&v)[VE], float (&lds)[NW][LX * VE])
 {
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, lx = lane % LX;
 #pragma unroll
@@ -333,29 +382,36 @@ __device__ __forceinline__ void column_sum(float (&v)[VE], float (*lds)[NW][LX *
     if (lane < LX)
 #pragma unroll
         for (int j = 0; j < VE; ++j)
-            (*lds)[w][lx * VE + j] = v[j];
+            lds[w][lx * VE + j] = v[j];
     __syncthreads();
 #pragma unroll
     for (int j = 0; j < VE; ++j) {
-        float s = (*lds)[0][lx * VE + j];
+        float s = lds[0][lx * VE + j];
         for (int i = 1; i < NW; ++i)
-            s += (*lds)[i][lx * VE + j];
+            s += lds[i][lx * VE + j];
         v[j] = s;
     }
 }
 
 template <typename D, int VE, int LX, int NW, int NP, bool CACHED>
-__global__ __launch_bounds__(NW * 64) void norm_fwd_planes(NormArgs a)
+__global__ __launch_bounds__(NW * 64, NP > 16 ? 4 : 1) void norm_fwd_planes(NormArgs a)
 {
     using T = typename D::T;
     using V = Vec<T, VE>;
     using P = Plane<VE, LX, NW>;
-    __shared__ float lds[1][NW][P::W];
+    __shared__ float lds[NW][P::W];
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, lx = lane % LX, ly = lane / LX;
     const int C = a.C, S = a.S, c0 = w * P::LY + ly;
     const float inv = 1.0f / (float)C;
     const int64_t cols = a.M * S, tiles = (cols + P::W - 1) / P::W;
-    for (int64_t t = blockIdx.x; t < tiles; t += gridDim.x) {
+    // the channels' weights: kept, or of 8 channels at a time where they are many
+    constexpr int NK = NP <= 16 ? NP : 8;
+    float gam[NK][1], bet[NK][1];
+    if constexpr (NK == NP) {
+        load_weights<1, NK>(a.gamma, 1.0f, c0, P::STEP, C, gam);
+        load_weights<1, NK>(a.beta, 0.0f, c0, P::STEP, C, bet);
+    }
+    for (int64_t t = first_tile(); t < tiles; t += gridDim.x) {
         const int64_t j = t * P::W + lx * VE;
         const bool live = j < cols;  // (VE divides S: a vector's columns are all live, in one m)
         const int64_t m = live ? j / S : 0;
@@ -365,18 +421,15 @@ __global__ __launch_bounds__(NW * 64) void norm_fwd_planes(NormArgs a)
         V keep[NP];
         float s[VE] = {}, q[VE] = {};
         if constexpr (CACHED) {
+            const int c1 = again(c0);
 #pragma unroll
-            for (int p = 0; p < NP; ++p) {
-                const int c = c0 + p * P::STEP;
-                keep[p] = V{};
-                if (live && c < C)
-                    keep[p] = *(const V*)(x + (int64_t)c * S);
-            }
+            for (int p = 0; p < NP; ++p)
+                keep[p] = *(const V*)(x + (int64_t)min(c1 + p * P::STEP, C - 1) * S);
 #pragma unroll
             for (int p = 0; p < NP; ++p)
 #pragma unroll
                 for (int i = 0; i < VE; ++i)
-                    s[i] += D::get(keep[p].v[i]);
+                    s[i] += c0 + p * P::STEP < C ? D::get(keep[p].v[i]) : 0.0f;
         } else if (live) {
             for (int c = c0; c < C; c += P::STEP) {
                 const V v = *(const V*)(x + (int64_t)c * S);
@@ -392,13 +445,14 @@ __global__ __launch_bounds__(NW * 64) void norm_fwd_planes(NormArgs a)
             mean[i] = s[i] * inv;
         if constexpr (CACHED) {
 #pragma unroll
-            for (int p = 0; p < NP; ++p)
-                if (c0 + p * P::STEP < C)
+            for (int p = 0; p < NP; ++p) {
+                again(keep[p]);
 #pragma unroll
-                    for (int i = 0; i < VE; ++i) {
-                        const float d = D::get(keep[p].v[i]) - mean[i];
-                        q[i] += d * d;
-                    }
+                for (int i = 0; i < VE; ++i) {
+                    const float d = D::get(keep[p].v[i]) - mean[i];
+                    q[i] += c0 + p * P::STEP < C ? d * d : 0.0f;
+                }
+            }
         } else if (live) {
             for (int c = c0; c < C; c += P::STEP) {
                 const V v = *(const V*)(x + (int64_t)c * S);
@@ -422,8 +476,7 @@ __global__ __launch_bounds__(NW * 64) void norm_fwd_planes(NormArgs a)
                 a.mean[j + i] = mean[i];
                 a.rstd[j + i] = rstd[i];
             }
-        const auto store = [&](int c, const V& in) {
-            const float g = a.gamma ? a.gamma[c] : 1.0f, b = a.beta ? a.beta[c] : 0.0f;
+        const auto store = [&](int c, const V& in, float g, float b) {
             V v;
 #pragma unroll
             for (int i = 0; i < VE; ++i)
@@ -431,13 +484,21 @@ __global__ __launch_bounds__(NW * 64) void norm_fwd_planes(NormArgs a)
             *(V*)(y + (int64_t)c * S) = v;
         };
         if constexpr (CACHED) {
+            const int c1 = again(c0);
 #pragma unroll
-            for (int p = 0; p < NP; ++p)
-                if (c0 + p * P::STEP < C)
-                    store(c0 + p * P::STEP, keep[p]);
+            for (int p = 0; p < NP; ++p) {
+                if constexpr (NK < NP)
+                    if (p % NK == 0) {
+                        load_weights<1, NK>(a.gamma, 1.0f, c1 + p * P::STEP, P::STEP, C, gam);
+                        load_weights<1, NK>(a.beta, 0.0f, c1 + p * P::STEP, P::STEP, C, bet);
+                    }
+                again(keep[p]);
+                if (c1 + p * P::STEP < C)
+                    store(c1 + p * P::STEP, keep[p], gam[p % NK][0], bet[p % NK][0]);
+            }
         } else {
             for (int c = c0; c < C; c += P::STEP)
-                store(c, *(const V*)(x + (int64_t)c * S));
+                store(c, *(const V*)(x + (int64_t)c * S), a.gamma ? a.gamma[c] : 1.0f, a.beta ? a.beta[c] : 0.0f);
         }
     }
 }
@@ -448,13 +509,14 @@ __global__ __launch_bounds__(NW * 64) void norm_bwd_planes(NormArgs a)
     using T = typename D::T;
     using V = Vec<T, VE>;
     using P = Plane<VE, LX, NW>;
-    __shared__ float lds[1][NW][P::W];
+    __shared__ float lds[NW][2 * P::W];
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, lx = lane % LX, ly = lane / LX;
     const int C = a.C, S = a.S, c0 = w * P::LY + ly;
     const float inv = 1.0f / (float)C;
     const int64_t cols = a.M * S, tiles = (cols + P::W - 1) / P::W;
-    float gg[NP] = {}, gb[NP] = {};
-    for (int64_t t = blockIdx.x; t < tiles; t += gridDim.x) {
+    float gg[NP] = {}, gb[NP] = {}, gam[NP][1];
+    load_weights<1, NP>(a.gamma, 1.0f, c0, P::STEP, C, gam);
+    for (int64_t t = first_tile(); t < tiles; t += gridDim.x) {
         const int64_t j = t * P::W + lx * VE;
         const bool live = j < cols;
         const int64_t m = live ? j / S : 0;
@@ -465,63 +527,63 @@ __global__ __launch_bounds__(NW * 64) void norm_bwd_planes(NormArgs a)
         float mean[VE], rstd[VE];
 #pragma unroll
         for (int i = 0; i < VE; ++i) {
-            mean[i] = live ? a.mean[j + i] : 0.0f;
-            rstd[i] = live ? a.rstd[j + i] : 0.0f;
+            mean[i] = a.mean[live ? j + i : 0];
+            rstd[i] = a.rstd[live ? j + i : 0];
         }
-        float sa[VE] = {}, sh[VE] = {};
-        const auto add = [&](int c, const V& vx, const V& vg, float& g1, float& g2) {
-            const float gam = a.gamma ? a.gamma[c] : 1.0f;
+        float sums[2 * VE] = {};  // of a, of a xh
+        const auto add = [&](const V& vx, const V& vg, float w, float& g1, float& g2) {
 #pragma unroll
             for (int i = 0; i < VE; ++i) {
                 const float g = D::get(vg.v[i]), xh = (D::get(vx.v[i]) - mean[i]) * rstd[i];
                 g1 += g * xh;
                 g2 += g;
-                sa[i] += g * gam;
-                sh[i] += g * gam * xh;
+                sums[i] += g * w;
+                sums[VE + i] += g * w * xh;
             }
         };
         V kx[NP], kg[NP];
         if constexpr (CACHED) {
+            const int c1 = again(c0);
 #pragma unroll
             for (int p = 0; p < NP; ++p) {
-                const int c = c0 + p * P::STEP;
-                if (live && c < C) {
-                    kx[p] = *(const V*)(x + (int64_t)c * S);
-                    kg[p] = *(const V*)(gy + (int64_t)c * S);
-                }
+                const int64_t at = (int64_t)min(c1 + p * P::STEP, C - 1) * S;
+                kx[p] = *(const V*)(x + at);
+                kg[p] = *(const V*)(gy + at);
             }
 #pragma unroll
             for (int p = 0; p < NP; ++p)
-                if (live && c0 + p * P::STEP < C)
-                    add(c0 + p * P::STEP, kx[p], kg[p], gg[p], gb[p]);
+                if (live && c1 + p * P::STEP < C)
+                    add(kx[p], kg[p], gam[p][0], gg[p], gb[p]);
         } else if (live) {
             for (int c = c0; c < C; c += P::STEP) {
                 float g1 = 0.0f, g2 = 0.0f;  // (the weights' sums are norm_bwd_planes_weights' there)
-                add(c, *(const V*)(x + (int64_t)c * S), *(const V*)(gy + (int64_t)c * S), g1, g2);
+                add(*(const V*)(x + (int64_t)c * S), *(const V*)(gy + (int64_t)c * S), a.gamma ? a.gamma[c] : 1.0f, g1, g2);
             }
         }
-        column_sum<VE, LX, NW>(sa, lds);
-        column_sum<VE, LX, NW>(sh, lds);
+        column_sum<2 * VE, LX, NW>(sums, lds);
         if (!live)
             continue;
-        const auto store = [&](int c, const V& vx, const V& vg) {
-            const float gam = a.gamma ? a.gamma[c] : 1.0f;
+        const auto store = [&](int c, const V& vx, const V& vg, float w) {
             V v;
 #pragma unroll
             for (int i = 0; i < VE; ++i) {
                 const float xh = (D::get(vx.v[i]) - mean[i]) * rstd[i];
-                v.v[i] = D::put(rstd[i] * (D::get(vg.v[i]) * gam - sa[i] * inv - xh * (sh[i] * inv)));
+                v.v[i] = D::put(rstd[i] * (D::get(vg.v[i]) * w - sums[i] * inv - xh * (sums[VE + i] * inv)));
             }
             *(V*)(gx + (int64_t)c * S) = v;
         };
         if constexpr (CACHED) {
+            const int c1 = again(c0);
 #pragma unroll
-            for (int p = 0; p < NP; ++p)
-                if (c0 + p * P::STEP < C)
-                    store(c0 + p * P::STEP, kx[p], kg[p]);
+            for (int p = 0; p < NP; ++p) {
+                again(kx[p]);
+                again(kg[p]);
+                if (c1 + p * P::STEP < C)
+                    store(c1 + p * P::STEP, kx[p], kg[p], gam[p][0]);
+            }
         } else {
             for (int c = c0; c < C; c += P::STEP)
-                store(c, *(const V*)(x + (int64_t)c * S), *(const V*)(gy + (int64_t)c * S));
+                store(c, *(const V*)(x + (int64_t)c * S), *(const V*)(gy + (int64_t)c * S), a.gamma ? a.gamma[c] : 1.0f);
         }
     }
     if constexpr (CACHED) {
@@ -570,24 +632,36 @@ __global__ __launch_bounds__(kT) void norm_bwd_planes_weights(NormArgs a)
     }
 }
 
-// grad_gamma, grad_beta from the blocks' partial sums: 16 threads a column,
+// grad_gamma, grad_beta from the blocks' partial sums: 64 threads a column,
 // joined in a fixed order
-__global__ __launch_bounds__(kT) void norm_weights_kernel(const float* __restrict__ part, int blocks, int C,
-                                                          float* __restrict__ gg, float* __restrict__ gb)
+__global__ __launch_bounds__(1024) void norm_weights_kernel(const float* __restrict__ part, int blocks, int C,
+                                                            float* __restrict__ gg, float* __restrict__ gb)
 {
-    __shared__ double lds[16][16];
+    __shared__ double lds[64][16];
     const int col = threadIdx.x & 15, row = threadIdx.x >> 4;
-    const int64_t e = (int64_t)blockIdx.x * 16 + col;  // 0 .. 2C-1
+    const int64_t e = (int64_t)blockIdx.x * 16 + col, last = 2 * (int64_t)C - 1;  // 0 .. 2C-1
+    const float* __restrict__ p = part + (e < last ? e : last);
     double s = 0.0;
-    if (e < 2 * (int64_t)C)
-        for (int b = row; b < blocks; b += 16)
-            s += (double)part[(int64_t)b * 2 * C + e];
+    for (int b0 = row; b0 < blocks; b0 += 64 * 8) {
+        float f[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            f[i] = p[(int64_t)min(b0 + 64 * i, blocks - 1) * 2 * C];
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            s += b0 + 64 * i < blocks ? (double)f[i] : 0.0;
+    }
     lds[row][col] = s;
     __syncthreads();
-    if (row != 0 || e >= 2 * (int64_t)C)
+    if (row >= 4)
         return;
     for (int r = 1; r < 16; ++r)
-        s += lds[r][col];
+        s += lds[row + 4 * r][col];
+    // (the four rows are in one wave)
+    s += __shfl_xor(s, 16);
+    s += __shfl_xor(s, 32);
+    if (row != 0 || e > last)
+        return;
     float* __restrict__ out = e < C ? gg : gb;
     if (out)
         out[e < C ? e : e - C] = (float)s;
@@ -623,26 +697,47 @@ bool launch_rows(const NormArgs& a, bool bwd, int blocks, hipStream_t s, hipErro
     return true;
 }
 
-template <typename D, int VE, int LX, int NW, int NP, bool CACHED>
-hipError_t planes(const NormArgs& a, bool bwd, int blocks, hipStream_t s)
+// The widest tile whose channels the registers of a block hold.  Tiles of 512
+// bytes a channel (64 lanes) rather than 128 where there are few channels: rows
+// that start at no cache line share two lines with the neighbouring tiles.
+template <typename D, int VE> hipError_t launch_planes(const NormArgs& a, bool bwd, int most, hipStream_t s, bool* cached)
 {
-    if (bwd)
-        norm_bwd_planes<D, VE, LX, NW, NP, CACHED><<<dim3(blocks), dim3(NW * 64), 0, s>>>(a);
-    else
-        norm_fwd_planes<D, VE, LX, NW, NP, CACHED><<<dim3(blocks), dim3(NW * 64), 0, s>>>(a);
-    return last();
-}
-
-template <typename D, int VE, int LX>
-hipError_t launch_planes(const NormArgs& a, bool bwd, int blocks, hipStream_t s, bool* cached)
-{
-    constexpr int LY = 64 / LX;
-    *cached = a.C <= 16 * 16 * LY;
-    if (a.C <= 4 * 16 * LY)
-        return planes<D, VE, LX, 4, 16, true>(a, bwd, blocks, s);
-    if (*cached)
-        return planes<D, VE, LX, 16, 16, true>(a, bwd, blocks, s);
-    return planes<D, VE, LX, 16, 1, false>(a, bwd, blocks, s);
+    constexpr int HALF = VE > 1 ? VE / 2 : 1;
+    const auto grid = [&](int width) {
+        const int64_t tiles = (a.M * a.S + width - 1) / width;
+        return dim3((unsigned)(bwd || tiles > most ? most : (tiles < 1 ? 1 : tiles)));
+    };
+    *cached = true;
+#define MFPSN_PLANES(VEC, LX, NW, NP, CACHED)                                                          \
+    do {                                                                                               \
+        if (bwd)                                                                                       \
+            norm_bwd_planes<D, VEC, LX, NW, NP, CACHED><<<grid(LX * VEC), dim3(NW * 64), 0, s>>>(a);   \
+        else                                                                                           \
+            norm_fwd_planes<D, VE, LX, NW, NP, CACHED><<<grid(LX * VE), dim3(NW * 64), 0, s>>>(a);     \
+        return last();                                                                                 \
+    } while (0)
+    if (a.C <= 16)
+        MFPSN_PLANES(VE, 64, 4, 4, true);
+    if (a.C <= 64)
+        MFPSN_PLANES(VE, 64, 4, 16, true);
+    if (a.C <= 128)
+        MFPSN_PLANES(VE, 32, 4, 16, true);
+    if constexpr (VE > 1) {
+        if (a.C <= 256)
+            MFPSN_PLANES(VE, 16, 4, 16, true);
+        if (a.C <= 512)
+            MFPSN_PLANES(VE, 16, 8, 16, true);
+        if (a.C <= 1024)  // (the backward keeps x, grad_y and three floats a channel: half as many columns)
+            MFPSN_PLANES(HALF, 16, 8, 32, true);
+    } else {
+        if (a.C <= 256)
+            MFPSN_PLANES(VE, 32, 8, 16, true);
+        if (a.C <= 512)
+            MFPSN_PLANES(VE, 32, 8, 32, true);
+    }
+    *cached = false;
+    MFPSN_PLANES(VE, 32, 16, 1, false);
+#undef MFPSN_PLANES
 }
 
 template <typename D> hipError_t run(const NormArgs& a, bool bwd, hipStream_t s)
@@ -655,7 +750,7 @@ template <typename D> hipError_t run(const NormArgs& a, bool bwd, hipStream_t s)
     bool whole = true;  // the kernel sums the weights' gradients too
     hipError_t err = hipSuccess;
     if (a.S == 1) {
-        const int grid = bwd ? blocks : (int)((a.M + 3) / 4 < (1 << 20) ? (a.M + 3) / 4 : (1 << 20));
+        const int grid = bwd ? blocks : (int)((a.M + 3) / 4 < 2048 ? (a.M + 3) / 4 : 2048);
         const bool done = a.C % VE == 0 && al(16) ? launch_rows<D, VE>(a, bwd, grid, s, &err)
                                                   : launch_rows<D, 1>(a, bwd, grid, s, &err);
         if (!done) {
@@ -668,10 +763,8 @@ template <typename D> hipError_t run(const NormArgs& a, bool bwd, hipStream_t s)
             err = last();
         }
     } else {
-        const int64_t tiles = (a.M * a.S + 63) / 64;
-        const int grid = bwd ? blocks : (int)(tiles < (1 << 20) ? tiles : (1 << 20));
-        err = a.S % 4 == 0 && al(4 * sizeof(typename D::T)) ? launch_planes<D, 4, 16>(a, bwd, grid, s, &whole)
-                                                            : launch_planes<D, 1, 64>(a, bwd, grid, s, &whole);
+        err = a.S % (VE / 2) == 0 && al(8) ? launch_planes<D, VE / 2>(a, bwd, bwd ? blocks : kNormMaxBlocks, s, &whole)
+                                           : launch_planes<D, 1>(a, bwd, bwd ? blocks : kNormMaxBlocks, s, &whole);
     }
     if (err != hipSuccess || !bwd || !a.part)
         return err;
@@ -683,7 +776,7 @@ template <typename D> hipError_t run(const NormArgs& a, bool bwd, hipStream_t s)
         if ((err = last()) != hipSuccess)
             return err;
     }
-    norm_weights_kernel<<<dim3((unsigned)((2 * (int64_t)a.C + 15) / 16)), dim3(kT), 0, s>>>(a.part, blocks, a.C, a.grad_gamma,
+    norm_weights_kernel<<<dim3((unsigned)((2 * (int64_t)a.C + 15) / 16)), dim3(1024), 0, s>>>(a.part, blocks, a.C, a.grad_gamma,
                                                                                         a.grad_beta);
     return last();
 }

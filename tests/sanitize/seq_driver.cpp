@@ -92,7 +92,7 @@ int main()
     EXPECT(mfpsn_layer_norm_workspace_size(4, 5, 6, nullptr), MFPSN_ERR_NULL);
     EXPECT(mfpsn_layer_norm_workspace_size(4, 5, -6, &n), MFPSN_ERR_SHAPE);
     EXPECT(mfpsn_layer_norm_workspace_size(1 << 30, 1000, 1, &n), MFPSN_OK);
-    CHECK(n == (size_t)mfpsn::kNormMaxBlocks * 2 * 1000 * 4);
+    CHECK(n == (size_t)mfpsn::norm_blocks(1 << 30, 1000, 1) * 2 * 1000 * 4 && n <= (size_t)mfpsn::kNormMaxBlocks * 8000);
     EXPECT(mfpsn_layer_norm_workspace_size(4, 5, 6, &n), MFPSN_OK);
     const auto bwd = [&](const void* x, float* gg, void* ws, size_t bytes) {
         return mfpsn_layer_norm_backward(4, 5, 6, MFPSN_F32, x, f, f, f, p, p, gg, nullptr, ws, bytes, nullptr);
