@@ -48,32 +48,38 @@ __global__ __launch_bounds__(256) void delta_steps_kernel(DeltaArgs a)
     const int v0 = (int)(blockIdx.x % vblocks) * kCols + lc * 4;
     const int len = a.lengths ? min(max(a.lengths[n], 0), a.T) : a.T;
 
+    // (reads behind the rows or columns go to the last of them: one under a condition is waited for by itself)
     float S[R][4];
+    if (a.state_in) {
+        float4 raw[R];
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
-        const int d = rg + kGroups * r;
-#pragma unroll
-        for (int c = 0; c < 4; ++c)
-            S[r][c] = 0.0f;
-        if (a.state_in && d < a.Dk) {
-            const float* p = a.state_in + (head * a.Dk + d) * a.Dv + v0;
+        for (int r = 0; r < R; ++r) {
+            const float* p = a.state_in + (head * a.Dk + min(rg + kGroups * r, a.Dk - 1)) * a.Dv;
             if (VEC) {
-                if (v0 < a.Dv) {
-                    const float4 f = *(const float4*)p;
-                    S[r][0] = f.x;
-                    S[r][1] = f.y;
-                    S[r][2] = f.z;
-                    S[r][3] = f.w;
-                }
+                raw[r] = *(const float4*)(p + min(v0, a.Dv - 4));
             } else {
-#pragma unroll
-                for (int c = 0; c < 4; ++c)
-                    if (v0 + c < a.Dv)
-                        S[r][c] = p[c];
+                raw[r].x = p[min(v0, a.Dv - 1)];
+                raw[r].y = p[min(v0 + 1, a.Dv - 1)];
+                raw[r].z = p[min(v0 + 2, a.Dv - 1)];
+                raw[r].w = p[min(v0 + 3, a.Dv - 1)];
             }
         }
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            const bool in = rg + kGroups * r < a.Dk;
+            S[r][0] = in ? raw[r].x : 0.0f;
+            S[r][1] = in ? raw[r].y : 0.0f;
+            S[r][2] = in ? raw[r].z : 0.0f;
+            S[r][3] = in ? raw[r].w : 0.0f;
+        }
+    } else {
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+            for (int c = 0; c < 4; ++c)
+                S[r][c] = 0.0f;
     }
-    float q[R], k[R], v[4], g, beta;
+    T q[R], k[R], v[4], g, beta;  // (as loaded: the next step's are on their way during this one)
     const auto fetch = [&](int t) {
         const int64_t row = (int64_t)t * a.N + n;
         const T* __restrict__ pq = (const T*)a.q + row * a.q_row + (int64_t)hk * a.Dk;
@@ -81,28 +87,42 @@ __global__ __launch_bounds__(256) void delta_steps_kernel(DeltaArgs a)
         const T* __restrict__ pv = (const T*)a.v + row * a.v_row + (int64_t)hv * a.Dv;
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-            const int d = rg + kGroups * r;
-            q[r] = d < a.Dk ? D::get(pq[d]) : 0.0f;
-            k[r] = d < a.Dk ? D::get(pk[d]) : 0.0f;
+            const int d = min(rg + kGroups * r, a.Dk - 1);
+            q[r] = pq[d];
+            k[r] = pk[d];
         }
 #pragma unroll
         for (int c = 0; c < 4; ++c)
-            v[c] = v0 + c < a.Dv ? D::get(pv[v0 + c]) : 0.0f;
-        g = D::get(((const T*)a.g)[row * a.Hv + hv]);
-        beta = D::get(((const T*)a.beta)[row * a.Hv + hv]);
+            v[c] = pv[min(v0 + c, a.Dv - 1)];
+        g = ((const T*)a.g)[row * a.Hv + hv];
+        beta = ((const T*)a.beta)[row * a.Hv + hv];
     };
     if (len > 0)
         fetch(0);
     for (int t = 0; t < len; ++t) {
         float sum[9] = {};  // S^T k, S^T q, k.q
+        float kf[R], vf[4];
+        const float decay = expf(D::get(g)), bf = D::get(beta);
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+            vf[c] = D::get(v[c]);
+        float qf[R];
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            const bool in = rg + kGroups * r < a.Dk;
+            qf[r] = in ? D::get(q[r]) : 0.0f;
+            kf[r] = in ? D::get(k[r]) : 0.0f;
+        }
+        if (t + 1 < len)
+            fetch(t + 1);
 #pragma unroll
         for (int r = 0; r < R; ++r) {
 #pragma unroll
             for (int c = 0; c < 4; ++c) {
-                sum[c] = __builtin_fmaf(S[r][c], k[r], sum[c]);
-                sum[4 + c] = __builtin_fmaf(S[r][c], q[r], sum[4 + c]);
+                sum[c] = __builtin_fmaf(S[r][c], kf[r], sum[c]);
+                sum[4 + c] = __builtin_fmaf(S[r][c], qf[r], sum[4 + c]);
             }
-            sum[8] = __builtin_fmaf(k[r], q[r], sum[8]);
+            sum[8] = __builtin_fmaf(kf[r], qf[r], sum[8]);
         }
 #pragma unroll
         for (int o = 8; o < 64; o <<= 1)
@@ -118,20 +138,17 @@ __global__ __launch_bounds__(256) void delta_steps_kernel(DeltaArgs a)
 #pragma unroll
         for (int i = 0; i < 9; ++i)
             sum[i] = (buf[0][i][lc] + buf[1][i][lc]) + (buf[2][i][lc] + buf[3][i][lc]);
-        const float decay = expf(g);
         float u[4], o[4];
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
-            u[c] = beta * (v[c] - decay * sum[c]);
+            u[c] = bf * (vf[c] - decay * sum[c]);
             o[c] = a.scale * __builtin_fmaf(sum[8], u[c], decay * sum[4 + c]);
         }
 #pragma unroll
         for (int r = 0; r < R; ++r)
 #pragma unroll
             for (int c = 0; c < 4; ++c)
-                S[r][c] = __builtin_fmaf(k[r], u[c], decay * S[r][c]);
-        if (t + 1 < len)
-            fetch(t + 1);
+                S[r][c] = __builtin_fmaf(kf[r], u[c], decay * S[r][c]);
         if (rg == 0) {
             T* __restrict__ po = (T*)a.o + (((int64_t)t * a.N + n) * a.Hv + hv) * a.Dv;
 #pragma unroll

@@ -12,6 +12,7 @@ autograd with the straight-through estimator of the quantizer (Sec. 4.2).
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 
@@ -632,11 +633,19 @@ def _shaped(t, dtype, device, shape, name):
         raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
 
 
+_NO_GUARD = contextlib.nullcontext()
+# (the current stream's handle without a Stream object around it, where torch has that: 2 us less a call)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
 def _on(device, stream):
-    """The device a call's tensors are on, as the current one, and the stream it goes to."""
+    """A guard that makes the tensors' device the current one, and the stream the call goes to."""
     if device.type != "cuda":
         raise ValueError(f"tensors must be on a GPU, got {device}")
-    return torch.cuda.device(device), stream if stream is not None else torch.cuda.current_stream(device)
+    guard = _NO_GUARD if device.index == torch.cuda.current_device() else torch.cuda.device(device)
+    if stream is None:
+        stream = _raw_stream(device.index) if _raw_stream else torch.cuda.current_stream(device)
+    return guard, stream
 
 
 def _norm_sizes(x, axis):
