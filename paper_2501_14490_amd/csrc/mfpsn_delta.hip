@@ -146,7 +146,7 @@ template <bool BF, int DKP> struct PrepLds {
 };
 
 template <typename D, bool BF, int DKP, bool VEC>
-__global__ __launch_bounds__(256) void delta_prep(DeltaArgs a)
+__global__ __launch_bounds__(256, 4) void delta_prep(DeltaArgs a)
 {
     using T = typename D::T;
     using M = Mat<BF>;
@@ -161,6 +161,9 @@ __global__ __launch_bounds__(256) void delta_prep(DeltaArgs a)
     if (live <= 0)
         return;
     const int64_t row0 = (int64_t)t0 * a.N + n;
+    // (a head's gates are on their way while the head before is computed)
+    const int64_t gate0 = (row0 + (int64_t)min(lane, live - 1) * a.N) * a.Hv + hk * group;
+    T gv = ((const T*)a.g)[gate0], bv = ((const T*)a.beta)[gate0];
     {
         Rows<D, El, DKP, 256, VEC> k, q;
         k.load((const T*)a.k + row0 * a.k_row + (int64_t)hk * a.Dk, a.k_step, live, a.Dk, a.near, tid);
@@ -192,15 +195,18 @@ __global__ __launch_bounds__(256) void delta_prep(DeltaArgs a)
         const int hv = hk * group + r;
         const int64_t unit = unit_of(a, n, hv, c);
         if (wave == 0) {
-            const int64_t at = (row0 + (int64_t)lane * a.N) * a.Hv + hv;
-            const double G = running_sum(lane < live ? decay_of(D::get(((const T*)a.g)[at])) : 0.0);
-            const float b = lane < live ? D::get(((const T*)a.beta)[at]) : 0.0f, eG = expf((float)G);
+            const double G = running_sum(lane < live ? decay_of(D::get(gv)) : 0.0);
+            const float b = lane < live ? D::get(bv) : 0.0f, eG = expf((float)G);
             s.G[lane] = G;
             s.beta[lane] = b;
             float* gate = a.gate + unit * 3 * L;
             gate[lane] = eG;
             gate[L + lane] = a.scale * eG;
             gate[2 * L + lane] = expf((float)(__shfl(G, 63) - G)) * b;
+        }
+        if (r + 1 < group) {
+            gv = ((const T*)a.g)[gate0 + r + 1];
+            bv = ((const T*)a.beta)[gate0 + r + 1];
         }
         __syncthreads();
         El* P = (El*)a.P + unit * L * L;
@@ -214,7 +220,7 @@ __global__ __launch_bounds__(256) void delta_prep(DeltaArgs a)
                 for (int e = 0; e < 4; ++e) {
                     const int j = j0 + e;
                     if (j <= i) {
-                        const float m = expf((float)(Gi - s.G[j])) * s.beta[j];
+                        const float m = fast_exp((float)(Gi - s.G[j])) * s.beta[j];
                         pv[e] = a.scale * m * kq[t][e];
                         av[e] = j < i ? m * kk[t][e] : 0.0f;
                     }
@@ -798,7 +804,7 @@ __global__ __launch_bounds__(512) void delta_grads(DeltaArgs a)
         nk.load((const T*)a.k + row0 * a.k_row + (int64_t)hk * a.Dk, a.k_step, live, a.Dk, a.near, tid);
         nq.load((const T*)a.q + row0 * a.q_row + (int64_t)hk * a.Dk, a.q_step, live, a.Dk, a.near, tid);
         for (int h = 0; h < group; ++h) {
-            const int tid = again(threadIdx.x);
+            const int tid = ONE ? (int)threadIdx.x : again(threadIdx.x);
             const int hv = hk * group + h;
             const int64_t unit = unit_of(a, n, hv, c);
             Rows<D, El, VB, 512, VEC> no, nd;
@@ -833,7 +839,7 @@ __global__ __launch_bounds__(512) void delta_grads(DeltaArgs a)
                 dX[t] = f32x4{0, 0, 0, 0};
             float z = 0.0f;  // <S0, dS1>
             for (int v0 = 0; v0 < a.dvp; v0 += VB) {
-                const int tid = again(threadIdx.x);
+                const int tid = ONE ? (int)threadIdx.x : again(threadIdx.x);
                 const int rows = min(VB, a.dvp - v0), cols = min(VB, a.Dv - v0);
                 __syncthreads();
                 if (h == 0 && v0 == 0) {
@@ -884,10 +890,7 @@ __global__ __launch_bounds__(512) void delta_grads(DeltaArgs a)
 #pragma unroll
                 for (int e = tid * 4; e < VB * DKP; e += 2048) {
                     const int at = s.v.S0.off(e / DKP, e % DKP);
-                    const El *p0 = s.v.S0.e + at, *p1 = s.v.dS.e + at;
-#pragma unroll
-                    for (int j = 0; j < 4; ++j)
-                        z = __builtin_fmaf(M::get(p0[j]), M::get(p1[j]), z);
+                    z = M::dot4(s.v.S0.e + at, s.v.dS.e + at, z);
                 }
             }
             __syncthreads();
@@ -921,7 +924,7 @@ __global__ __launch_bounds__(512) void delta_grads(DeltaArgs a)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         const int j = M::at(t, g) + e;
-                        const float m = j <= i - half ? expf((float)(Gi - s.G[j])) : 0.0f;
+                        const float m = j <= i - half ? fast_exp((float)(Gi - s.G[j])) : 0.0f;
                         const float f = (half ? -m : a.scale * m) * dX[t][e], b = s.beta[j], both = f * kx[t][e];
                         y[e] = j < i ? both : 0.0f;
                         diag += j == i ? both : 0.0f;  // (one lane of the four that have step i)
@@ -929,10 +932,8 @@ __global__ __launch_bounds__(512) void delta_grads(DeltaArgs a)
                         w[e] = f * b;
                     }
 #pragma unroll
-                    for (int o = 1; o < 16; o <<= 1)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            y[e] += __shfl_xor(y[e], o);
+                    for (int e = 0; e < 4; ++e)
+                        y[e] = sum16(y[e]);
                 }
                 if (col == 0)
                     *(f32x4*)(s.sum[wave8] + M::at(t, g)) = y;

@@ -33,7 +33,25 @@ __device__ __forceinline__ int again(int t)
     return t;
 }
 
+// e^x by v_exp_f32 (2^x).  The rounding of x log2 e makes it off by |x| 2^-24
+// relative, so by at most 2^-24 / e of the largest, 1, of the decays' factors.
+__device__ __forceinline__ float fast_exp(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504088896f); }
+
+// Sum over the 16 lanes of a result's columns, in every lane
+__device__ __forceinline__ float sum16(float v)
+{
+#define MFPSN_ROR(n) \
+    v += __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), 0x120 + (n), 0xf, 0xf, true))
+    MFPSN_ROR(8);
+    MFPSN_ROR(4);
+    MFPSN_ROR(2);
+    MFPSN_ROR(1);
+#undef MFPSN_ROR
+    return v;
+}
+
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef short i16x4 __attribute__((ext_vector_type(4)));
@@ -87,6 +105,15 @@ template <> struct Mat<false> {
     __device__ static f32x4 mma(Frag a, Frag b, f32x4 c) { return mfma_f32(a, b, c); }
     __device__ static El put(float v) { return v; }
     __device__ static float get(El v) { return v; }
+    // sum of four neighbours' products, added to c
+    __device__ static float dot4(const El* p, const El* q, float c)
+    {
+        const f32x4 a = *(const f32x4*)p, b = *(const f32x4*)q;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            c = __builtin_fmaf(a[i], b[i], c);
+        return c;
+    }
 };
 
 template <> struct Mat<true> {
@@ -129,6 +156,12 @@ template <> struct Mat<true> {
     __device__ static f32x4 mma(Frag a, Frag b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
     __device__ static El put(float v) { return (__bf16)v; }
     __device__ static float get(El v) { return (float)v; }
+    __device__ static float dot4(const El* p, const El* q, float c)
+    {
+        const bf16x4 a = *(const bf16x4*)p, b = *(const bf16x4*)q;
+        c = __builtin_amdgcn_fdot2_f32_bf16(bf16x2{a[0], a[1]}, bf16x2{b[0], b[1]}, c, false);
+        return __builtin_amdgcn_fdot2_f32_bf16(bf16x2{a[2], a[3]}, bf16x2{b[2], b[3]}, c, false);
+    }
 };
 
 // An LDS tile of ROWS x COLS elements.  bf16: rows follow each other without
