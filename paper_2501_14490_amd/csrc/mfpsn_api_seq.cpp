@@ -63,6 +63,12 @@ DeltaLayout layout_of(const mfpsn_delta_desc* d)
     return delta_layout(d->T, d->N, d->Hv, d->Dk, d->Dv, delta_elem(d->dtype));
 }
 
+size_t segment_bytes(const mfpsn_delta_desc* d, size_t* local)
+{
+    return delta_segment_bytes((int64_t)d->N * d->Hv, (d->Dv + 15) / 16 * 16,
+                               ((int64_t)d->T + kDeltaChunk - 1) / kDeltaChunk, (size_t)delta_dkp(d->Dk), local);
+}
+
 bool by_steps(const mfpsn_delta_desc* d) { return d->T <= kDeltaStepsMaxT; }
 
 // rows that may be read 16 bytes at a time: the base and every row and head
@@ -229,7 +235,8 @@ int mfpsn_delta_workspace_size(const mfpsn_delta_desc* desc, size_t* bytes)
         return st;
     if (!bytes)
         return MFPSN_ERR_NULL;
-    *bytes = by_steps(desc) ? 0 : layout_of(desc).chunk_bytes();
+    size_t local;
+    *bytes = by_steps(desc) ? 0 : layout_of(desc).chunk_bytes() + segment_bytes(desc, &local);
     return MFPSN_OK;
 }
 
@@ -275,8 +282,10 @@ int mfpsn_delta_forward(const mfpsn_delta_desc* desc, const void* q, const void*
         return MFPSN_ERR_ALIGN;
     const DeltaLayout l = layout_of(desc);
     const bool steps = !saved && by_steps(desc);
+    size_t local = 0;
+    const size_t segments = saved || steps ? 0 : segment_bytes(desc, &local);
     if (saved ? (saved_bytes < l.saved_bytes() || !aligned(saved, 16))
-              : (!steps && (!workspace || workspace_bytes < l.chunk_bytes() || !aligned(workspace, 16))))
+              : (!steps && (!workspace || workspace_bytes < l.chunk_bytes() + segments || !aligned(workspace, 16))))
         return MFPSN_ERR_WORKSPACE;
     DeltaArgs a;
     fill(a, desc, q, k, v, g, beta, lengths);
@@ -287,6 +296,14 @@ int mfpsn_delta_forward(const mfpsn_delta_desc* desc, const void* q, const void*
     a.vec_v = wide_rows(v, a.v_row, desc->Dv, es) && wide_rows(o, (int64_t)desc->Hv * desc->Dv, desc->Dv, es);
     if (!steps)
         place(a, l, saved ? saved : workspace, saved != nullptr);
+    a.nseg = 1;
+    a.seg_chunks = a.nc;
+    if (segments > 0) {
+        a.nseg = delta_segments((int64_t)a.N * a.Hv * ((a.dvp + 63) / 64), a.nc);
+        a.seg_chunks = (a.nc + a.nseg - 1) / a.nseg;
+        a.local = (float*)((char*)workspace + l.chunk_bytes());
+        a.start = (float*)((char*)workspace + l.chunk_bytes() + local);
+    }
     const hipStream_t s = (hipStream_t)stream;
     return (steps ? launch_delta_steps(a, desc->dtype, s) : launch_delta_forward(a, desc->dtype, s)) == hipSuccess
                ? MFPSN_OK

@@ -32,6 +32,10 @@ struct DeltaArgs {
     // per (sequence, value head, chunk), see delta_layout
     void *X, *P, *S0, *U;         // S0, U: nullable in the forward (not saved)
     float* gate;                  // [3][64]: e^G, scale e^G, e^(G_last - G) beta
+    // long sequences of few heads: cut into segments (delta_segments)
+    int32_t nseg, seg_chunks;     // 1 and nc where there is one
+    float* local;                 // [head][nseg][dkp][64 vblocks + dkp]: a segment's state from zeros, its transition
+    float* start;                 // [head][nseg][dkp][64 vblocks]: the state before each segment
     // backward
     const void* grad_o;
     const float* grad_state_out;  // nullable: zeros
@@ -54,6 +58,34 @@ struct DeltaLayout {
 inline int delta_elem(int dtype) { return dtype == 1 ? 2 : 4; }
 
 inline int delta_dkp(int Dk) { return Dk <= 64 ? 64 : 128; }
+
+// Segments of a forward over `blocks` blocks (sequences x value heads x 64
+// columns) and nc chunks.  A block walks its chunks one after the other, 3.4 us
+// each (bf16, Dk = Dv = 128), and 256 CUs take a block each, so few heads leave
+// most of the chip idle.  With S segments the chunks are walked three times (for
+// the states without and the transitions, then for the outputs), but in S places at once,
+// and the segments' states are joined in order (4 us a segment): worth it from
+// four segments on, of 16 chunks at least.
+inline int delta_segments(int64_t blocks, int64_t nc)
+{
+    if (blocks < 1 || blocks > 64)
+        return 1;
+    int64_t s = 256 / blocks;
+    s = s < nc / 16 ? s : nc / 16;
+    if (s < 4)
+        return 1;
+    const int64_t each = (nc + s - 1) / s;
+    return (int)((nc + each - 1) / each);
+}
+
+// Bytes of the segments' states (local, start) of a forward, 0 without segments
+inline size_t delta_segment_bytes(int64_t heads, int64_t dvp, int64_t nc, size_t dkp, size_t* local)
+{
+    const size_t vcols = (size_t)(dvp + 63) / 64 * 64;
+    const int s = delta_segments(heads * (int64_t)(vcols / 64), nc);
+    *local = s > 1 ? (size_t)heads * s * dkp * (vcols + dkp) * sizeof(float) : 0;
+    return s > 1 ? *local + (size_t)heads * s * dkp * vcols * sizeof(float) : 0;
+}
 
 // es: delta_elem
 inline DeltaLayout delta_layout(int64_t T, int64_t N, int64_t Hv, int Dk, int Dv, int es)

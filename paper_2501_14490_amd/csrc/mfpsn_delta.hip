@@ -268,7 +268,12 @@ template <bool BF, int DKP> struct ScanLds {
     alignas(16) float gate[3 * L];
 };
 
-template <typename D, bool BF, int DKP, int NW, bool VEC>
+//
+// With segments (a.nseg > 1) a block walks one of them, from its state in
+// a.start.  STATES: what those are made of, a segment's state from zeros in the
+// blocks of the values' columns, and in the blocks behind them its transition:
+// the columns of the identity, walked without values (r = -X diag(e^G) K S0).
+template <typename D, bool BF, int DKP, int NW, bool VEC, bool STATES>
 __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(1, 1))) void delta_scan(DeltaArgs a)
 {
     using T = typename D::T;
@@ -280,20 +285,28 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(1, 1)))
     static_assert(NW == 4 && TH >= 3 * L);
     __shared__ Lds s;
     const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, col = lane & 15, g = lane >> 4;
-    const int vblocks = (a.dvp + 16 * NW - 1) / (16 * NW);
-    const int64_t head = blockIdx.x / vblocks;
+    const int vblocks = (a.dvp + 63) / 64, blocks = STATES ? vblocks + DKP / 64 : vblocks;
+    const int vb = (int)(blockIdx.x % blocks), seg = (int)(blockIdx.x / blocks % a.nseg);
+    const int64_t head = blockIdx.x / blocks / a.nseg;
+    const bool values = !STATES || vb < vblocks;
     const int n = (int)(head / a.Hv), hv = (int)(head - (int64_t)n * a.Hv), hk = hv / (a.Hv / a.Hk);
-    const int v0 = (int)(blockIdx.x % vblocks) * 64, vl = M::at(wave, col >> 2) + (col & 3), v = v0 + vl, cols = min(64, a.Dv - v0);
+    const int v0 = vb * 64, vl = M::at(wave, col >> 2) + (col & 3), v = v0 + vl, cols = min(64, a.Dv - v0);
     const bool mine = v < a.Dv;         // a column of the tensors
     const bool wide = v < a.dvp;        // a column of the padded arrays
-    const int len = length_of(a, n), chunks = (len + L - 1) / L;
+    const int len = length_of(a, n), all = (len + L - 1) / L;
+    const int first = min(seg * a.seg_chunks, all), chunks = min(first + a.seg_chunks, all);
     f32x4 S[TK];
 #pragma unroll
     for (int t = 0; t < TK; ++t)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
             const int d = M::at(t, g) + r;
-            S[t][r] = a.state_in && mine && d < a.Dk ? a.state_in[(head * a.Dk + d) * a.Dv + v] : 0.0f;
+            if (STATES)
+                S[t][r] = !values && d == v - vblocks * 64 ? 1.0f : 0.0f;
+            else if (a.nseg > 1)
+                S[t][r] = a.start[((head * a.nseg + seg) * DKP + d) * (vblocks * 64) + v];
+            else
+                S[t][r] = a.state_in && mine && d < a.Dk ? a.state_in[(head * a.Dk + d) * a.Dv + v] : 0.0f;
         }
     Rows<D, El, DKP, TH, VEC> nk, nq;
     Rows<D, El, 64, TH, VEC> nv;
@@ -305,7 +318,7 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(1, 1)))
         const int64_t row0 = (int64_t)t0 * a.N + n, unit = unit_of(a, n, hv, c);
         if (part == 0)
             nk.load((const T*)a.k + row0 * a.k_row + (int64_t)hk * a.Dk, a.k_step, live, a.Dk, a.near, tid);
-        if (part == 1)
+        if (part == 1 && !STATES)
             nq.load((const T*)a.q + row0 * a.q_row + (int64_t)hk * a.Dk, a.q_step, live, a.Dk, a.near, tid);
         if (part == 2) {
             nx[0].load((const El*)a.X + unit * L * L * (BF ? 2 : 1), L, tid);
@@ -313,29 +326,37 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(1, 1)))
                 nx[1].load((const El*)a.X + unit * L * L * 2 + L * L, L, tid);
         }
         if (part == 3) {
-            np.load((const El*)a.P + unit * L * L, L, tid);
-            nv.load((const T*)a.v + row0 * a.v_row + (int64_t)hv * a.Dv + v0, a.v_step, live, cols, a.near, tid);
+            if (!STATES)
+                np.load((const El*)a.P + unit * L * L, L, tid);
+            if (values)
+                nv.load((const T*)a.v + row0 * a.v_row + (int64_t)hv * a.Dv + v0, a.v_step, live, cols, a.near, tid);
             ngate = a.gate[unit * 3 * L + min(tid, 3 * L - 1)];
         }
     };
-    if (chunks > 0)
+    if (!values)
+        for (int i = tid; i < (int)(sizeof(s.v.e) / sizeof(El)); i += TH)
+            s.v.e[i] = M::put(0.0f);
+    if (first < chunks)
 #pragma unroll
         for (int part = 0; part < 4; ++part)
-            fetch(0, part, tid);
-    for (int c = 0; c < chunks; ++c) {
+            fetch(first, part, tid);
+    for (int c = first; c < chunks; ++c) {
         const int t0 = c * L, live = min(L, len - t0);
         const int64_t row0 = (int64_t)t0 * a.N + n, unit = unit_of(a, n, hv, c);
         __syncthreads();
         nk.store(s.k, live, a.Dk, tid);
-        nq.store(s.q, live, a.Dk, tid);
+        if (!STATES)
+            nq.store(s.q, live, a.Dk, tid);
         nx[0].store(s.x[0], L, tid);
         if constexpr (BF)
             nx[1].store(s.x[1], L, tid);
-        np.store(s.p, L, tid);
+        if (!STATES)
+            np.store(s.p, L, tid);
         if (tid < 3 * L)
             s.gate[tid] = ngate;
-        nv.store(s.v, live, cols, tid);
-        if (c > 0)  // the chunk before, whose outputs wait in LDS
+        if (values)
+            nv.store(s.v, live, cols, tid);
+        if (!STATES && c > first)  // the chunk before, whose outputs wait in LDS
             store_rows<M, D, VEC>(s.o, (T*)a.o + ((row0 - (int64_t)L * a.N) * a.Hv + hv) * a.Dv + v0, a.o_step, L, cols,
                                   again(threadIdx.x));
         __syncthreads();
@@ -352,7 +373,8 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(1, 1)))
 #pragma unroll
             for (int t = 0; t < 4; ++t) {
                 fk[u & 1][t] = M::rows(s.k, t, u, tid);
-                fq[u & 1][t] = M::rows(s.q, t, u, tid);
+                if (!STATES)
+                    fq[u & 1][t] = M::rows(s.q, t, u, tid);
             }
         };
 #pragma unroll
@@ -391,14 +413,16 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(1, 1)))
 #pragma unroll
             for (int t = 0; t < 4; ++t) {
                 KS[t] = M::mma(fk[u & 1][t], b, KS[t]);
-                O[t] = M::mma(fq[u & 1][t], b, O[t]);
+                if (!STATES)
+                    O[t] = M::mma(fq[u & 1][t], b, O[t]);
             }
             if constexpr (BF) {
                 const Frag rest = M::pack_rest(S + u * TU, b);
 #pragma unroll
                 for (int t = 0; t < 4; ++t) {
                     KS[t] = M::mma(fk[u & 1][t], rest, KS[t]);
-                    O[t] = M::mma(fq[u & 1][t], rest, O[t]);
+                    if (!STATES)
+                        O[t] = M::mma(fq[u & 1][t], rest, O[t]);
                 }
             }
             in_order();
@@ -408,7 +432,7 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(1, 1)))
             fv[w] = M::cols(s.v, wave, w, tid);
 #pragma unroll
             for (int t = 0; t < 4; ++t)
-                if (M::reaches(w * TU, t))
+                if (!STATES && M::reaches(w * TU, t))
                     fp[w][t] = M::rows(s.p, t, w, tid);
         }
         in_order();
@@ -454,6 +478,7 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(1, 1)))
                 *(Frag*)(pu + u * KU) = M::pack(U + u * TU);
         }
         // outputs
+        if constexpr (!STATES) {
 #pragma unroll
         for (int u = 0; u < UL; ++u) {
             const Frag b = M::pack(U + u * TU);
@@ -468,6 +493,7 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(1, 1)))
                     if (M::reaches(u * TU, t))
                         O[t] = M::mma(fp[u][t], rest, O[t]);
             }
+        }
         }
         // the state behind the chunk
         const float last = s.gate[L - 1];
@@ -498,20 +524,32 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(1, 1)))
             }
             in_order();
         }
+        if (!STATES)
 #pragma unroll
-        for (int u = 0; u < UL; ++u)
-            *(Frag*)(s.o.e + s.o.off(vl, u * KU + M::at(0, g))) = M::pack(O + u * TU);
+            for (int u = 0; u < UL; ++u)
+                *(Frag*)(s.o.e + s.o.off(vl, u * KU + M::at(0, g))) = M::pack(O + u * TU);
     }
-    if (chunks > 0) {  // the last chunk's outputs
+    if constexpr (STATES) {
+        float* local = a.local + (head * a.nseg + seg) * DKP * (blocks * 64) + v;
+#pragma unroll
+        for (int t = 0; t < TK; ++t)
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                local[(M::at(t, g) + r) * (blocks * 64)] = S[t][r];
+        return;
+    }
+    if (first < chunks) {  // the last chunk's outputs
         __syncthreads();
         const int64_t row0 = (int64_t)(chunks - 1) * L * a.N + n;
-        store_rows<M, D, VEC>(s.o, (T*)a.o + (row0 * a.Hv + hv) * a.Dv + v0, a.o_step, len - (chunks - 1) * L, cols, tid);
+        store_rows<M, D, VEC>(s.o, (T*)a.o + (row0 * a.Hv + hv) * a.Dv + v0, a.o_step, min(L, len - (chunks - 1) * L), cols, tid);
     }
     if (!mine)
         return;
-    for (int t = len + (lane >> 4); t < a.T; t += 4)  // steps behind the sequence's end
-        ((T*)a.o)[(((int64_t)t * a.N + n) * a.Hv + hv) * a.Dv + v] = D::put(0.0f);
-    if (a.state_out)
+    // the segment's steps behind the sequence's end
+    const int64_t end = min((int64_t)a.T, (int64_t)(seg + 1) * a.seg_chunks * L);
+    for (int64_t t = max((int64_t)len, (int64_t)seg * a.seg_chunks * L) + g; t < end; t += 4)
+        ((T*)a.o)[((t * a.N + n) * a.Hv + hv) * a.Dv + v] = D::put(0.0f);
+    if (a.state_out && seg == a.nseg - 1)
 #pragma unroll
         for (int t = 0; t < TK; ++t)
 #pragma unroll
@@ -520,6 +558,58 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(1, 1)))
                 if (d < a.Dk)
                     a.state_out[(head * a.Dk + d) * a.Dv + v] = S[t][r];
             }
+}
+
+// The states before the segments of a head, in order: S <- T S + local, in float.
+// A wave has 16 columns, as in the scan; T comes through LDS.
+template <int DKP> __global__ __launch_bounds__(256) void delta_join(DeltaArgs a)
+{
+    using M = Mat<false>;
+    constexpr int TK = DKP / 16;
+    __shared__ Tile<float, DKP, DKP> s;
+    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, g = lane >> 4;
+    const int vblocks = (a.dvp + 63) / 64, width = vblocks * 64 + DKP;
+    const int64_t head = blockIdx.x / vblocks;
+    const int v = (int)(blockIdx.x % vblocks) * 64 + 16 * wave + (lane & 15);
+    f32x4 S[TK];
+#pragma unroll
+    for (int t = 0; t < TK; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int d = M::at(t, g) + r;
+            S[t][r] = a.state_in && v < a.Dv && d < a.Dk ? a.state_in[(head * a.Dk + d) * a.Dv + v] : 0.0f;
+        }
+    for (int seg = 0; seg < a.nseg; ++seg) {
+        float* start = a.start + (head * a.nseg + seg) * DKP * (vblocks * 64) + v;
+        const float* local = a.local + (head * a.nseg + seg) * DKP * width;
+#pragma unroll
+        for (int t = 0; t < TK; ++t)
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                start[(M::at(t, g) + r) * (vblocks * 64)] = S[t][r];
+        if (seg + 1 == a.nseg)
+            break;
+        __syncthreads();
+        for (int i = tid * 4; i < DKP * DKP; i += 1024)
+            *(f32x4*)(s.e + s.off(i / DKP, i % DKP)) = *(const f32x4*)(local + (i / DKP) * width + vblocks * 64 + i % DKP);
+        f32x4 next[TK];
+#pragma unroll
+        for (int t = 0; t < TK; ++t)
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                next[t][r] = local[(M::at(t, g) + r) * width + v];
+        __syncthreads();
+#pragma unroll
+        for (int u = 0; u < TK; ++u) {
+            const f32x4 b = M::pack(S + u);
+#pragma unroll
+            for (int t = 0; t < TK; ++t)
+                next[t] = M::mma(M::rows(s, t, u, tid), b, next[t]);
+        }
+#pragma unroll
+        for (int t = 0; t < TK; ++t)
+            S[t] = next[t];
+    }
 }
 
 // The chunks in reverse, in the same manner: the gradient of the state, the
@@ -1067,7 +1157,19 @@ template <typename D, bool BF, int DKP, bool VEC> hipError_t forward(const Delta
         if (err != hipSuccess)
             return err;
     }
-    delta_scan<D, BF, DKP, kScanWaves, VEC><<<dim3((unsigned)scan_blocks(a)), dim3(kScanWaves * 64), 0, s>>>(a);
+    const int64_t heads = (int64_t)a.N * a.Hv, vblocks = (a.dvp + 63) / 64;
+    const dim3 threads(kScanWaves * 64);
+    if (a.nseg > 1) {
+        delta_scan<D, BF, DKP, kScanWaves, VEC, true>
+            <<<dim3((unsigned)(heads * a.nseg * (vblocks + DKP / 64))), threads, 0, s>>>(a);
+        hipError_t err = hipGetLastError();
+        if (err != hipSuccess)
+            return err;
+        delta_join<DKP><<<dim3((unsigned)(heads * vblocks)), dim3(256), 0, s>>>(a);
+        if ((err = hipGetLastError()) != hipSuccess)
+            return err;
+    }
+    delta_scan<D, BF, DKP, kScanWaves, VEC, false><<<dim3((unsigned)(heads * a.nseg * vblocks)), threads, 0, s>>>(a);
     return hipGetLastError();
 }
 

@@ -126,6 +126,25 @@ def test_long_sequence_and_slow_decay(dtype):
     check(make(600, 1, 1, 1, 128, 128, dtype, seed=4, rate=0.004), state=False, grad_state=False)
 
 
+# long enough, and of few enough heads, for the sequence to be cut into segments whose states are joined: ends within a
+# segment, sequences that end before most segments, keys and values of one and of several tiles, states in and out
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("T,N,Hk,Hv,Dk,Dv,lengths", [(4200, 1, 1, 1, 16, 24, None), (5000, 3, 1, 2, 20, 70, [5000, 130, 0]),
+                                                     (4161, 1, 1, 2, 128, 16, None)])
+def test_segments_of_a_long_sequence(T, N, Hk, Hv, Dk, Dv, lengths, dtype):
+    c = make(T, N, Hk, Hv, Dk, Dv, dtype, seed=T, lengths=lengths, rate=0.003)
+    if lengths:
+        for n in range(N):
+            for name in NAMES:
+                c[name][lengths[n]:, n] = float("nan")
+    o64, S64 = ref.delta(*[c[n].double() for n in NAMES], c["scale"], c["state"].double(), c["lengths"])
+    desc, ins, (o, S) = forward(c)
+    plain = mfpsn.make_delta_desc((T, 1000, Hk, Dk), (T, 1000, Hv, Dv), dtype)  # (too many heads: not cut)
+    assert mfpsn.mfpsn_delta_workspace_size(desc) > mfpsn.mfpsn_delta_workspace_size(plain) / 1000 * N
+    near(o, o64, BOUND[dtype]["o"], "o")
+    near(S, S64, BOUND[dtype]["state"], "state")
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("T,lengths", [(150, [150, 0, 1, 64, 65, 149]), (6, [6, 0, 3, 1, 5, 2]), (70, [0, 0, 0, 0, 0, 0]),
                                        (64, [64, 200, -3, 63, 1, 32])])
