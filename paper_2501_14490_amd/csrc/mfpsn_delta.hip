@@ -274,7 +274,7 @@ template <bool BF, int DKP> struct ScanLds {
 // blocks of the values' columns, and in the blocks behind them its transition:
 // the columns of the identity, walked without values (r = -X diag(e^G) K S0).
 template <typename D, bool BF, int DKP, int NW, bool VEC, bool STATES>
-__global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(1, 1))) void delta_scan(DeltaArgs a)
+__global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(BF && STATES ? 2 : 1, BF && STATES ? 2 : 1))) void delta_scan(DeltaArgs a)
 {
     using T = typename D::T;
     using M = Mat<BF>;
@@ -561,17 +561,38 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(1, 1)))
 }
 
 // The states before the segments of a head, in order: S <- T S + local, in float.
-// A wave has 16 columns, as in the scan; T comes through LDS.
+// A wave has 16 columns, as in the scan; T comes through LDS, the next segment's
+// in four parts while this one's is multiplied with.
 template <int DKP> __global__ __launch_bounds__(256) void delta_join(DeltaArgs a)
 {
     using M = Mat<false>;
-    constexpr int TK = DKP / 16;
-    __shared__ Tile<float, DKP, DKP> s;
+    constexpr int TK = DKP / 16, PARTS = 4, NL = DKP * DKP / 4 / 256 / PARTS;
+    __shared__ Tile<float, DKP, DKP> s[2];
     const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, g = lane >> 4;
     const int vblocks = (a.dvp + 63) / 64, width = vblocks * 64 + DKP;
     const int64_t head = blockIdx.x / vblocks;
     const int v = (int)(blockIdx.x % vblocks) * 64 + 16 * wave + (lane & 15);
-    f32x4 S[TK];
+    f32x4 S[TK], part[NL];
+    const auto load = [&](int seg, int p) {
+        const float* T = a.local + (head * a.nseg + seg) * DKP * width + vblocks * 64;
+#pragma unroll
+        for (int n = 0; n < NL; ++n) {
+            const int i = ((p * NL + n) * 256 + tid) * 4;
+            part[n] = *(const f32x4*)(T + (i / DKP) * width + i % DKP);
+        }
+    };
+    const auto store = [&](int buf, int p) {
+#pragma unroll
+        for (int n = 0; n < NL; ++n) {
+            const int i = ((p * NL + n) * 256 + tid) * 4;
+            *(f32x4*)(s[buf].e + s[buf].off(i / DKP, i % DKP)) = part[n];
+        }
+    };
+#pragma unroll
+    for (int p = 0; p < PARTS; ++p) {
+        load(0, p);
+        store(0, p);
+    }
 #pragma unroll
     for (int t = 0; t < TK; ++t)
 #pragma unroll
@@ -581,7 +602,7 @@ template <int DKP> __global__ __launch_bounds__(256) void delta_join(DeltaArgs a
         }
     for (int seg = 0; seg < a.nseg; ++seg) {
         float* start = a.start + (head * a.nseg + seg) * DKP * (vblocks * 64) + v;
-        const float* local = a.local + (head * a.nseg + seg) * DKP * width;
+        const float* local = a.local + (head * a.nseg + seg) * DKP * width + v;
 #pragma unroll
         for (int t = 0; t < TK; ++t)
 #pragma unroll
@@ -590,25 +611,31 @@ template <int DKP> __global__ __launch_bounds__(256) void delta_join(DeltaArgs a
         if (seg + 1 == a.nseg)
             break;
         __syncthreads();
-        for (int i = tid * 4; i < DKP * DKP; i += 1024)
-            *(f32x4*)(s.e + s.off(i / DKP, i % DKP)) = *(const f32x4*)(local + (i / DKP) * width + vblocks * 64 + i % DKP);
-        f32x4 next[TK];
+        f32x4 next[TK], own[TK];
 #pragma unroll
-        for (int t = 0; t < TK; ++t)
+        for (int t = 0; t < TK; ++t) {
+            next[t] = f32x4{0, 0, 0, 0};
 #pragma unroll
             for (int r = 0; r < 4; ++r)
-                next[t][r] = local[(M::at(t, g) + r) * width + v];
-        __syncthreads();
+                own[t][r] = local[(M::at(t, g) + r) * width];
+        }
 #pragma unroll
-        for (int u = 0; u < TK; ++u) {
-            const f32x4 b = M::pack(S + u);
+        for (int p = 0; p < PARTS; ++p) {
+            if (seg + 2 < a.nseg)
+                load(seg + 1, p);
 #pragma unroll
-            for (int t = 0; t < TK; ++t)
-                next[t] = M::mma(M::rows(s, t, u, tid), b, next[t]);
+            for (int u = p * TK / PARTS; u < (p + 1) * TK / PARTS; ++u) {
+                const f32x4 b = M::pack(S + u);
+#pragma unroll
+                for (int t = 0; t < TK; ++t)
+                    next[t] = M::mma(M::rows(s[seg & 1], t, u, tid), b, next[t]);
+            }
+            if (seg + 2 < a.nseg)
+                store((seg + 1) & 1, p);
         }
 #pragma unroll
         for (int t = 0; t < TK; ++t)
-            S[t] = next[t];
+            S[t] = next[t] + own[t];
     }
 }
 
