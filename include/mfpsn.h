@@ -406,8 +406,9 @@ int mfpsn_layer_norm_backward(int64_t M, int32_t C, int32_t S, int32_t dtype, co
  * The rule is stable for beta |k|^2 <= 2 (unit keys, beta in [0, 1]).
  * Arithmetic: the state is float; MFPSN_F32 products are float, MFPSN_BF16 ones
  * are 16-bit matrix products summed in float, of which those that make the next
- * state take their operands as sums of two 16-bit numbers (the state is as
- * exact as float products make it), the others round them once.  A value that is
+ * state take their operands as sums of three 16-bit numbers (the state is as
+ * exact as float products make it), the others round an operand once (the
+ * outputs', the state and the residuals, to 16 of their bits).  A value that is
  * not finite spoils its own and the later outputs of its sequence and head and,
  * in the whole-sequence form, those of the 64 steps around it (a chunk).
  *

@@ -44,8 +44,8 @@ struct DeltaArgs {
     float* grad_state_in;         // nullable
 };
 
-// Bytes a (sequence, value head, chunk) takes of each array: X (16-bit: a high
-// and a low part), P, the gates; U and S0 (what the backward needs besides).
+// Bytes a (sequence, value head, chunk) takes of each array: X (16-bit: as the
+// sum of three), P, the gates; U and S0 (what the backward needs besides).
 struct DeltaLayout {
     size_t units;                     // sequences x value heads x chunks
     size_t x, p, gate, u, s0;         // bytes of each unit
@@ -93,7 +93,7 @@ inline DeltaLayout delta_layout(int64_t T, int64_t N, int64_t Hv, int Dk, int Dv
     DeltaLayout l;
     const size_t L = kDeltaChunk, dvp = (size_t)(Dv + 15) / 16 * 16, dkp = (size_t)delta_dkp(Dk);
     l.units = (size_t)N * (size_t)Hv * (size_t)((T + kDeltaChunk - 1) / kDeltaChunk);
-    l.x = L * L * 4;
+    l.x = L * L * (size_t)(es == 2 ? 3 * 2 : 4);
     l.p = L * L * (size_t)es;
     l.gate = 3 * L * 4;
     l.u = dvp * L * (size_t)es;

@@ -152,6 +152,7 @@ __global__ __launch_bounds__(256, 4) void delta_prep(DeltaArgs a)
     using M = Mat<BF>;
     using El = typename M::El;
     using Lds = PrepLds<BF, DKP>;
+    constexpr int NX = BF ? 3 : 1;
     __shared__ Lds s;
     const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, col = lane & 15, g = lane >> 4;
     const int c = blockIdx.x % a.nc;
@@ -230,19 +231,18 @@ __global__ __launch_bounds__(256, 4) void delta_prep(DeltaArgs a)
         }
         __syncthreads();
         unit_lower_inverse(s.A, s.X);
-        // 16-bit: X as the sum of two numbers of 8 bits each (the scan's products need it as exactly as float)
-        El* X = (El*)a.X + unit * L * L * (BF ? 2 : 1);
+        // 16-bit: X as the sum of three numbers of 8 bits each (the scan's products need it as exactly as float)
+        El* X = (El*)a.X + unit * L * L * NX;
         for (int e = tid * 4; e < L * L; e += 1024) {
             const f32x4 x = *(const f32x4*)(s.X + (e / L) * LF + e % L);
             if constexpr (BF) {
-                bf16x4 hi, lo;
+                f32x4 rest = x;
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    hi[j] = (__bf16)x[j];
-                    lo[j] = (__bf16)(x[j] - (float)hi[j]);
+                for (int n = 0; n < 3; ++n) {
+                    const bf16x4 h = __builtin_convertvector(rest, bf16x4);
+                    *(bf16x4*)(X + n * L * L + e) = h;
+                    rest -= __builtin_convertvector(h, f32x4);
                 }
-                *(bf16x4*)(X + e) = hi;
-                *(bf16x4*)(X + L * L + e) = lo;
             } else {
                 *(f32x4*)(X + e) = x;
             }
@@ -259,12 +259,23 @@ __global__ __launch_bounds__(256, 4) void delta_prep(DeltaArgs a)
 // a SIMD (the state, the operands of the next products and the next tiles
 // take more than half of the registers), so nothing but the order of its own
 // instructions hides a wave's latencies: operands are read a group ahead.
-template <bool BF, int DKP> struct ScanLds {
+template <bool BF, int DKP, bool STATES> struct ScanLds {
     using El = typename Mat<BF>::El;
     Tile<El, L, DKP> k, q;
-    Tile<El, L, L> x[BF ? 2 : 1], p;
+    Tile<El, L, L> x[BF ? 3 : 1], p;
     Tile<El, L, 64> v;  // [i][v]
     Tile<El, 64, L> o;  // [v][i]
+    alignas(16) float gate[3 * L];
+};
+template <bool BF, int DKP> struct ScanLds<BF, DKP, true> {  // (no outputs: no Q, P, O; their names for tiles of their types)
+    using El = typename Mat<BF>::El;
+    union {
+        Tile<El, L, DKP> k, q;
+    };
+    Tile<El, L, L> x[BF ? 3 : 1];
+    union {
+        Tile<El, L, 64> v, p, o;
+    };
     alignas(16) float gate[3 * L];
 };
 
@@ -280,8 +291,10 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(BF && S
     using M = Mat<BF>;
     using El = typename M::El;
     using Frag = typename M::Frag;
-    using Lds = ScanLds<BF, DKP>;
-    constexpr int TK = DKP / 16, TH = NW * 64, KU = M::KU, TU = M::TU, UK = DKP / KU, UL = L / KU;
+    using Lds = ScanLds<BF, DKP, STATES>;
+    constexpr int TK = DKP / 16, TH = NW * 64, KU = M::KU, TU = M::TU, UK = DKP / KU, UL = L / KU, NX = BF ? 3 : 1;
+    // operands of X read ahead: all, or the first where two waves share a SIMD (and hide each other's reads)
+    constexpr int XA = BF && STATES ? 1 : UL;
     static_assert(NW == 4 && TH >= 3 * L);
     __shared__ Lds s;
     const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, col = lane & 15, g = lane >> 4;
@@ -310,7 +323,7 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(BF && S
         }
     Rows<D, El, DKP, TH, VEC> nk, nq;
     Rows<D, El, 64, TH, VEC> nv;
-    Dense<El, L, L, TH> nx[BF ? 2 : 1], np;
+    Dense<El, L, L, TH> nx[NX], np;
     float ngate;
     // The chunk's tiles in four parts (a wave waits where it issues more reads than the memory pipe takes)
     const auto fetch = [&](int c, int part, int tid) {
@@ -321,9 +334,9 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(BF && S
         if (part == 1 && !STATES)
             nq.load((const T*)a.q + row0 * a.q_row + (int64_t)hk * a.Dk, a.q_step, live, a.Dk, a.near, tid);
         if (part == 2) {
-            nx[0].load((const El*)a.X + unit * L * L * (BF ? 2 : 1), L, tid);
-            if constexpr (BF)
-                nx[1].load((const El*)a.X + unit * L * L * 2 + L * L, L, tid);
+#pragma unroll
+            for (int n = 0; n < NX; ++n)
+                nx[n].load((const El*)a.X + (unit * NX + n) * L * L, L, tid);
         }
         if (part == 3) {
             if (!STATES)
@@ -347,9 +360,9 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(BF && S
         nk.store(s.k, live, a.Dk, tid);
         if (!STATES)
             nq.store(s.q, live, a.Dk, tid);
-        nx[0].store(s.x[0], L, tid);
-        if constexpr (BF)
-            nx[1].store(s.x[1], L, tid);
+#pragma unroll
+        for (int n = 0; n < NX; ++n)
+            nx[n].store(s.x[n], L, tid);
         if (!STATES)
             np.store(s.p, L, tid);
         if (tid < 3 * L)
@@ -366,9 +379,10 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(BF && S
             for (int u = 0; u < UK; ++u)
                 *(Frag*)(S0 + u * KU) = M::pack(S + u * TU);
         }
-        // K S0 and Q S0.  16-bit: the state goes in as the sum of two numbers of 8 bits each.
+        // K S0 and Q S0.  16-bit: K S0 makes the next state, so the state goes in as the sum of three numbers of 8 bits
+        // each, all of its float; for the outputs, which are rounded to 8 bits, as two.
         f32x4 R[4], KS[4], O[4], eG[4], sG[4], gam[4];
-        Frag fv[UL], fk[2][4], fq[2][4], fx[UL][4], fl[UL][4], fp[UL][4], ft[2][TK];
+        Frag fv[UL], fk[2][4], fq[2][4], fx[NX][UL][4], fp[UL][4], ft[2][TK];
         const auto read_kq = [&](int u) {
 #pragma unroll
             for (int t = 0; t < 4; ++t) {
@@ -376,6 +390,15 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(BF && S
                 if (!STATES)
                     fq[u & 1][t] = M::rows(s.q, t, u, tid);
             }
+        };
+        // (X and P are lower triangular)
+        const auto read_x = [&](int w) {
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+                if (M::reaches(w * TU, t))
+#pragma unroll
+                    for (int n = 0; n < NX; ++n)
+                        fx[n][w][t] = M::rows(s.x[n], t, w, tid);
         };
 #pragma unroll
         for (int t = 0; t < 4; ++t)
@@ -399,32 +422,20 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(BF && S
                     gam[t] = *(const f32x4*)(s.gate + 2 * L + M::at(t, g));
                 }
 #pragma unroll
-                for (int w = 0; w < UL; ++w)
-#pragma unroll
-                    for (int t = 0; t < 4; ++t)
-                        if (M::reaches(w * TU, t)) {  // (X and P are lower triangular)
-                            fx[w][t] = M::rows(s.x[0], t, w, tid);
-                            if constexpr (BF)
-                                fl[w][t] = M::rows(s.x[1], t, w, tid);
-                        }
+                for (int w = 0; w < XA; ++w)
+                    read_x(w);
             }
             in_order();
-            const Frag b = M::pack(S + u * TU);
+            Frag b[NX];
+            M::split(S + u * TU, b);
 #pragma unroll
-            for (int t = 0; t < 4; ++t) {
-                KS[t] = M::mma(fk[u & 1][t], b, KS[t]);
-                if (!STATES)
-                    O[t] = M::mma(fq[u & 1][t], b, O[t]);
-            }
-            if constexpr (BF) {
-                const Frag rest = M::pack_rest(S + u * TU, b);
+            for (int n = 0; n < NX; ++n)
 #pragma unroll
                 for (int t = 0; t < 4; ++t) {
-                    KS[t] = M::mma(fk[u & 1][t], rest, KS[t]);
-                    if (!STATES)
-                        O[t] = M::mma(fq[u & 1][t], rest, O[t]);
+                    KS[t] = M::mma(fk[u & 1][t], b[n], KS[t]);
+                    if (!STATES && n < 2)
+                        O[t] = M::mma(fq[u & 1][t], b[n], O[t]);
                 }
-            }
             in_order();
         }
 #pragma unroll
@@ -449,19 +460,21 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(BF && S
         }
 #pragma unroll
         for (int u = 0; u < UL; ++u) {
-            const Frag b = M::pack(R + u * TU);
-            Frag rest;
-            if constexpr (BF)
-                rest = M::pack_rest(R + u * TU, b);
+            if (u >= XA) {
+                in_order();
+                read_x(u);
+                in_order();
+            }
+            Frag b[NX];
+            M::split(R + u * TU, b);
 #pragma unroll
-            for (int t = 0; t < 4; ++t)
-                if (M::reaches(u * TU, t)) {
-                    U[t] = M::mma(fx[u][t], b, U[t]);
-                    if constexpr (BF) {
-                        U[t] = M::mma(fx[u][t], rest, U[t]);
-                        U[t] = M::mma(fl[u][t], b, U[t]);
-                    }
-                }
+            for (int n = 0; n < NX; ++n)  // (products of parts m and n with m + n < 3: the others are below float's rounding)
+#pragma unroll
+                for (int m = 0; m < NX - n; ++m)
+#pragma unroll
+                    for (int t = 0; t < 4; ++t)
+                        if (M::reaches(u * TU, t))
+                            U[t] = M::mma(fx[m][u][t], b[n], U[t]);
         }
         const auto read_kt = [&](int u) {
 #pragma unroll
@@ -480,20 +493,16 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(BF && S
         // outputs
         if constexpr (!STATES) {
 #pragma unroll
-        for (int u = 0; u < UL; ++u) {
-            const Frag b = M::pack(U + u * TU);
+            for (int u = 0; u < UL; ++u) {
+                Frag b[BF ? 2 : 1];
+                M::split(U + u * TU, b);
 #pragma unroll
-            for (int t = 0; t < 4; ++t)
-                if (M::reaches(u * TU, t))
-                    O[t] = M::mma(fp[u][t], b, O[t]);
-            if constexpr (BF) {
-                const Frag rest = M::pack_rest(U + u * TU, b);
+                for (int n = 0; n < (BF ? 2 : 1); ++n)
 #pragma unroll
-                for (int t = 0; t < 4; ++t)
-                    if (M::reaches(u * TU, t))
-                        O[t] = M::mma(fp[u][t], rest, O[t]);
+                    for (int t = 0; t < 4; ++t)
+                        if (M::reaches(u * TU, t))
+                            O[t] = M::mma(fp[u][t], b[n], O[t]);
             }
-        }
         }
         // the state behind the chunk
         const float last = s.gate[L - 1];
@@ -512,16 +521,13 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(BF && S
             if (u + 1 < UL)
                 read_kt(u + 1);
             in_order();
-            const Frag b = M::pack(U + u * TU);
+            Frag b[NX];
+            M::split(U + u * TU, b);
 #pragma unroll
-            for (int t = 0; t < TK; ++t)
-                S[t] = M::mma(ft[u & 1][t], b, S[t]);
-            if constexpr (BF) {
-                const Frag rest = M::pack_rest(U + u * TU, b);
+            for (int n = 0; n < NX; ++n)
 #pragma unroll
                 for (int t = 0; t < TK; ++t)
-                    S[t] = M::mma(ft[u & 1][t], rest, S[t]);
-            }
+                    S[t] = M::mma(ft[u & 1][t], b[n], S[t]);
             in_order();
         }
         if (!STATES)
@@ -688,7 +694,7 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(1, 1)))
         if (part == 1)
             nq.load((const T*)a.q + row0 * a.q_row + (int64_t)hk * a.Dk, a.q_step, live, a.Dk, a.near, tid);
         if (part == 2) {
-            nx.load((const El*)a.X + unit * L * L * (BF ? 2 : 1), L, tid);
+            nx.load((const El*)a.X + unit * L * L * (BF ? 3 : 1), L, tid);
             np.load((const El*)a.P + unit * L * L, L, tid);
         }
         if (part == 3) {

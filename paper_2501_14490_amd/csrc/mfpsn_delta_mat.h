@@ -102,6 +102,7 @@ template <> struct Mat<false> {
         return f32x4{s.e[Tile::off(k, m)], s.e[Tile::off(k + 1, m)], s.e[Tile::off(k + 2, m)], s.e[Tile::off(k + 3, m)]};
     }
     __device__ static Frag pack(const f32x4* t) { return t[0]; }
+    template <int N> __device__ static void split(const f32x4* t, Frag (&f)[N]) { f[0] = t[0]; }
     __device__ static f32x4 mma(Frag a, Frag b, f32x4 c) { return mfma_f32(a, b, c); }
     __device__ static El put(float v) { return v; }
     __device__ static float get(El v) { return v; }
@@ -143,15 +144,20 @@ template <> struct Mat<true> {
     {
         return __builtin_convertvector(__builtin_shufflevector(t[0], t[1], 0, 1, 2, 3, 4, 5, 6, 7), Frag);
     }
-    // what pack() left of each value, as the next 8 bits
-    __device__ static Frag pack_rest(const f32x4* t, Frag hi)
+    // a value as the sum of N numbers of 8 bits each (three hold all of a float's)
+    template <int N> __device__ static void split(const f32x4* t, Frag (&f)[N])
     {
-        const u32x4 h = __builtin_bit_cast(u32x4, hi);
-        f32x8 f;
+        f32x8 x = __builtin_shufflevector(t[0], t[1], 0, 1, 2, 3, 4, 5, 6, 7);
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-            f[i] = t[i >> 2][i & 3] - __builtin_bit_cast(float, i & 1 ? h[i >> 1] & 0xffff0000u : h[i >> 1] << 16);
-        return __builtin_convertvector(f, Frag);
+        for (int n = 0; n < N; ++n) {
+            f[n] = __builtin_convertvector(x, Frag);
+            if (n + 1 == N)
+                break;
+            const u32x4 h = __builtin_bit_cast(u32x4, f[n]);
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                x[i] -= __builtin_bit_cast(float, i & 1 ? h[i >> 1] & 0xffff0000u : h[i >> 1] << 16);
+        }
     }
     __device__ static f32x4 mma(Frag a, Frag b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
     __device__ static El put(float v) { return (__bf16)v; }

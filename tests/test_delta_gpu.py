@@ -7,8 +7,8 @@ Bounds, in the 2-norm of an output over all its values (B times the norm of what
   bf16  one half step, 2^-8, for each rounding to 16 bits on the way: o has four (state, residuals, P, the stored o);
         grad_v five (state's gradient, dO is exact, P, r', X, the stored value); grad_q, grad_k six (both states, r,
         E or F, dV, the stored value); grad_g and grad_beta eight (the same, as differences of two such sums).
-        States and their gradients are float: the forward's keeps 16 bits through each of five products, 5 * 2^-16,
-        besides the float bound; the gradient of the first state is made of grad_v's roundings.
+        States and their gradients are float: the forward's has the float bound (its products take all 24 bits); the
+        gradient of the first state is made of grad_v's roundings.
 Single values: 40 times that bound times the larger of their size and the output's root mean square."""
 import math
 
@@ -29,7 +29,7 @@ DT = {"f32": torch.float32, "bf16": torch.bfloat16}
 HALF = 2.0 ** -8
 F32 = 1e-4
 BOUND = {"f32": dict.fromkeys(("o", "state", "q", "k", "v", "g", "beta", "state_in"), F32),
-         "bf16": {"o": 4 * HALF, "state": 5 * 2.0 ** -16 + F32, "q": 6 * HALF, "k": 6 * HALF, "v": 5 * HALF,
+         "bf16": {"o": 4 * HALF, "state": F32, "q": 6 * HALF, "k": 6 * HALF, "v": 5 * HALF,
                   "g": 8 * HALF, "beta": 8 * HALF, "state_in": 5 * HALF}}
 NAMES = ("q", "k", "v", "g", "beta")
 
