@@ -14,6 +14,7 @@ from __future__ import annotations
 
 import contextlib
 import ctypes
+import math
 import os
 
 import torch
@@ -339,8 +340,9 @@ def mfpsn_delta_backward(desc: MfpsnDeltaDesc, q, k, v, g, beta, lengths, saved,
 
 
 def mfpsn_delta_step(desc: MfpsnDeltaDesc, q, k, v, g, beta, state_in, o, state_out, stream=None) -> None:
-    _check(_lib.mfpsn_delta_step(ctypes.byref(desc), _ptr(q), _ptr(k), _ptr(v), _ptr(g), _ptr(beta), _ptr(state_in),
-                                 _ptr(o), _ptr(state_out), _stream(stream)), "mfpsn_delta_step")
+    _check(_lib.mfpsn_delta_step(ctypes.byref(desc), q.data_ptr(), k.data_ptr(), v.data_ptr(), g.data_ptr(),
+                                 beta.data_ptr(), state_in.data_ptr() if state_in is not None else None, o.data_ptr(),
+                                 state_out.data_ptr(), _stream(stream)), "mfpsn_delta_step")
 
 
 # ---------------------------------------------------------------------------
@@ -628,6 +630,8 @@ def _float_dtype(t, name):
 
 
 def _shaped(t, dtype, device, shape, name):
+    if t.dtype is dtype and t.shape == shape and t.device == device and t.is_contiguous():
+        return
     _expect(t, dtype, device, name)
     if tuple(t.shape) != tuple(shape):
         raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
@@ -652,12 +656,7 @@ def _norm_sizes(x, axis):
     if not -x.dim() <= axis < x.dim():
         raise ValueError(f"axis {axis} is none of x's {x.dim()}")
     axis %= x.dim()
-    M, S = 1, 1
-    for n in x.shape[:axis]:
-        M *= int(n)
-    for n in x.shape[axis + 1:]:
-        S *= int(n)
-    return M, int(x.shape[axis]), S
+    return math.prod(x.shape[:axis]), x.shape[axis], math.prod(x.shape[axis + 1:])
 
 
 def layer_norm_forward(x, gamma=None, beta=None, eps: float = 1e-5, axis: int = 2, want_stats: bool = False,
@@ -670,9 +669,10 @@ def layer_norm_forward(x, gamma=None, beta=None, eps: float = 1e-5, axis: int = 
     dt = _float_dtype(x, "x")
     _expect(x, x.dtype, dev, "x")
     M, C, S = _norm_sizes(x, axis)
-    for t, name in ((gamma, "gamma"), (beta, "beta")):
-        if t is not None:
-            _shaped(t, torch.float32, dev, (C,), name)
+    if gamma is not None:
+        _shaped(gamma, torch.float32, dev, (C,), "gamma")
+    if beta is not None:
+        _shaped(beta, torch.float32, dev, (C,), "beta")
     guard, stream = _on(dev, stream)
     with guard:
         y = torch.empty_like(x)
@@ -756,8 +756,10 @@ def make_delta_desc(qk_shape, v_shape, dtype="f32", scale=None) -> MfpsnDeltaDes
 
 
 def _delta_row(t, dtype, device, shape, name):
-    """Elements between the rows (t, n) of a [T, N, H, D] tensor whose rows are dense: a dense tensor's, or those of
-    a slice of a projection's output."""
+    """Elements between the rows (t, n) of a [T, N, H, D] tensor whose rows [H, D] are dense, as those of a slice of a
+    projection's output; 0 for a dense tensor."""
+    if t.dtype is dtype and t.shape == shape and t.device == device and t.is_contiguous():
+        return 0
     if t.dtype != dtype:
         raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
     if t.device != device:
@@ -765,8 +767,6 @@ def _delta_row(t, dtype, device, shape, name):
     if tuple(t.shape) != tuple(shape):
         raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
     T, N, H, D = shape
-    if t.is_contiguous():
-        return H * D
     row = t.stride(1) if N > 1 else t.stride(0)
     if (D > 1 and t.stride(3) != 1) or (H > 1 and t.stride(2) != D) or (T > 1 and t.stride(0) != N * row) or row < H * D:
         raise ValueError(f"{name} of strides {t.stride()} must have dense rows [H, D] at equal distances")
@@ -778,17 +778,15 @@ def _delta_inputs(desc, q, k, v, g, beta, lengths, step=False):
     if desc.dtype not in (MFPSN_F32, MFPSN_BF16):
         raise TypeError("the delta rule is for f32 and bf16")
     dev, st = q.device, STORAGE[desc.dtype]
-    T = 1 if step else desc.T
-    d = MfpsnDeltaDesc.from_buffer_copy(desc)
-    d.T = T
-    d.q_row = _delta_row(q, st, dev, (T, desc.N, desc.Hk, desc.Dk), "q")
-    d.k_row = _delta_row(k, st, dev, (T, desc.N, desc.Hk, desc.Dk), "k")
-    d.v_row = _delta_row(v, st, dev, (T, desc.N, desc.Hv, desc.Dv), "v")
-    for t, name in ((g, "g"), (beta, "beta")):
-        _shaped(t, st, dev, (T, desc.N, desc.Hv), name)
+    T, N, Hk, Hv, Dk, Dv = 1 if step else desc.T, desc.N, desc.Hk, desc.Hv, desc.Dk, desc.Dv
+    qk, gate = (T, N, Hk, Dk), (T, N, Hv)
+    rows = (_delta_row(q, st, dev, qk, "q"), _delta_row(k, st, dev, qk, "k"),
+            _delta_row(v, st, dev, (T, N, Hv, Dv), "v"))
+    _shaped(g, st, dev, gate, "g")
+    _shaped(beta, st, dev, gate, "beta")
     if lengths is not None:
-        _shaped(lengths, torch.int32, dev, (desc.N,), "lengths")
-    return d
+        _shaped(lengths, torch.int32, dev, (N,), "lengths")
+    return MfpsnDeltaDesc(T, N, Hk, Hv, Dk, Dv, desc.dtype, desc.scale, *rows)
 
 
 def _delta_state(desc, t, device, name):
