@@ -874,14 +874,18 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(1, 1)))
 }
 
 // The gradients of a chunk's queries, keys, decays and write strengths, for
-// one key head.  All products are computed transposed: waves w and w + 4 have
-// the columns i = 16 w .. 16 w + 15 (steps) of every result, so a step's
-// factors are one value a lane; each of the two has half of the keys' rows,
-// and one of the matrices E, F that the products of the second part share
-// through LDS.  8 waves, two a SIMD.
-template <bool BF, int DKP> struct GradsLds {
+// one key head.  All products are computed transposed: a wave has 16 steps i,
+// the columns of every result, so a step's factors are one value a lane.  The
+// matrices E, F go to the products of the second part through LDS.
+//
+// ONE: every key head has one value head.  bf16 then takes four waves and 32
+// values at a time (NH = 2: a wave has both halves of the keys' rows, E and F),
+// so that two blocks share a CU and one computes while the other waits for its
+// reads.  Otherwise the sums over the heads need registers besides, and float
+// tiles the LDS: eight waves, waves w and w + 4 with the same steps, each with
+// half of the keys' rows and one of E and F.
+template <bool BF, int DKP, int VB> struct GradsLds {
     using El = typename Mat<BF>::El;
-    static constexpr int VB = BF ? 64 : 32;  // values staged at a time
     Tile<El, L, DKP> k, q;
     union {
         struct {
@@ -898,20 +902,23 @@ template <bool BF, int DKP> struct GradsLds {
     float z[8];
 };
 
-// ONE: every key head has one value head (nothing is summed over heads, so the
-// sums need no registers of their own while a head is computed)
+template <bool BF, bool ONE> struct GradsShape {
+    static constexpr int NH = BF && ONE ? 2 : 1, THREADS = NH == 2 ? 256 : 512, VB = NH == 2 ? 32 : (BF ? 64 : 32);
+};
+
 template <typename D, bool BF, int DKP, bool VEC, bool ONE>
-__global__ __launch_bounds__(512) void delta_grads(DeltaArgs a)
+__global__ __launch_bounds__((GradsShape<BF, ONE>::THREADS), 2) void delta_grads(DeltaArgs a)
 {
     using T = typename D::T;
     using M = Mat<BF>;
     using El = typename M::El;
     using Frag = typename M::Frag;
-    using Lds = GradsLds<BF, DKP>;
-    constexpr int TH = DKP / 32, KU = M::KU, UK = DKP / KU, UL = L / KU, VB = Lds::VB;
+    constexpr int NH = GradsShape<BF, ONE>::NH, THREADS = GradsShape<BF, ONE>::THREADS, VB = GradsShape<BF, ONE>::VB;
+    using Lds = GradsLds<BF, DKP, VB>;
+    constexpr int TH = DKP / 32 * NH, KU = M::KU, UK = DKP / KU, UL = L / KU;
     __shared__ Lds s;
     const int tid = threadIdx.x, wave8 = tid >> 6, lane = tid & 63, col = lane & 15, g = lane >> 4;
-    const int wave = wave8 & 3, half = wave8 >> 2;
+    const int wave = wave8 & 3, half = wave8 >> 2, dt = half * TH;  // (half: 0 where NH = 2)
     const int c = blockIdx.x % a.nc;
     const int64_t nh = blockIdx.x / a.nc;
     const int n = (int)(nh / a.Hk), hk = (int)(nh - (int64_t)n * a.Hk), group = ONE ? 1 : a.Hv / a.Hk;
@@ -923,16 +930,16 @@ __global__ __launch_bounds__(512) void delta_grads(DeltaArgs a)
     for (int t = 0; t < TH; ++t)
         dq[t] = dk[t] = f32x4{0, 0, 0, 0};
     if (live > 0) {
-        Rows<D, El, DKP, 512, VEC> nk, nq;
+        Rows<D, El, DKP, THREADS, VEC> nk, nq;
         nk.load((const T*)a.k + row0 * a.k_row + (int64_t)hk * a.Dk, a.k_step, live, a.Dk, a.near, tid);
         nq.load((const T*)a.q + row0 * a.q_row + (int64_t)hk * a.Dk, a.q_step, live, a.Dk, a.near, tid);
         for (int h = 0; h < group; ++h) {
             const int tid = ONE ? (int)threadIdx.x : again(threadIdx.x);
             const int hv = hk * group + h;
             const int64_t unit = unit_of(a, n, hv, c);
-            Rows<D, El, VB, 512, VEC> no, nd;
-            Dense<El, VB, L, 512> nr;
-            Dense<El, VB, DKP, 512> n0, n1;
+            Rows<D, El, VB, THREADS, VEC> no, nd;
+            Dense<El, VB, L, THREADS> nr;
+            Dense<El, VB, DKP, THREADS> n0, n1;
             const auto fetch = [&](int v0, int tid) {
                 const int rows = min(VB, a.dvp - v0), cols = min(VB, a.Dv - v0);
                 const int64_t at = (row0 * a.Hv + hv) * a.Dv + v0;
@@ -953,13 +960,15 @@ __global__ __launch_bounds__(512) void delta_grads(DeltaArgs a)
                 s.to_end[lane] = expf((float)(__shfl(G, 63) - G));
             }
             // products over the values: with the states (the half's keys), and r dO^T or r dV^T
-            f32x4 qs[TH], ks[TH], ws[TH], dX[4];
+            f32x4 qs[TH], ks[TH], ws[TH], dX[NH][4];
 #pragma unroll
             for (int t = 0; t < TH; ++t)
                 qs[t] = ks[t] = ws[t] = f32x4{0, 0, 0, 0};
 #pragma unroll
-            for (int t = 0; t < 4; ++t)
-                dX[t] = f32x4{0, 0, 0, 0};
+            for (int n = 0; n < NH; ++n)
+#pragma unroll
+                for (int t = 0; t < 4; ++t)
+                    dX[n][t] = f32x4{0, 0, 0, 0};
             float z = 0.0f;  // <S0, dS1>
             for (int v0 = 0; v0 < a.dvp; v0 += VB) {
                 const int tid = ONE ? (int)threadIdx.x : again(threadIdx.x);
@@ -985,7 +994,7 @@ __global__ __launch_bounds__(512) void delta_grads(DeltaArgs a)
                     Frag ar[4], as[TH];
 #pragma unroll
                     for (int t = 0; t < TH; ++t)
-                        as[t] = M::cols(s.v.S0, half * TH + t, u, tid);
+                        as[t] = M::cols(s.v.S0, dt + t, u, tid);
 #pragma unroll
                     for (int t = 0; t < 4; ++t)
                         ar[t] = M::cols(s.v.r, t, u, tid);
@@ -998,77 +1007,94 @@ __global__ __launch_bounds__(512) void delta_grads(DeltaArgs a)
                     in_order();
 #pragma unroll
                     for (int t = 0; t < TH; ++t)
-                        as[t] = M::cols(s.v.dS, half * TH + t, u, tid);
+                        as[t] = M::cols(s.v.dS, dt + t, u, tid);
                     in_order();
-                    const Frag bx = half ? bv : bo;
 #pragma unroll
-                    for (int t = 0; t < 4; ++t)
-                        if (M::reaches(t, wave))
-                            dX[t] = M::mma(ar[t], bx, dX[t]);
+                    for (int n = 0; n < NH; ++n) {
+                        const Frag bx = (NH == 2 ? n : half) ? bv : bo;
+#pragma unroll
+                        for (int t = 0; t < 4; ++t)
+                            if (M::reaches(t, wave))
+                                dX[n][t] = M::mma(ar[t], bx, dX[n][t]);
+                    }
 #pragma unroll
                     for (int t = 0; t < TH; ++t)
                         ws[t] = M::mma(as[t], br, ws[t]);
                     in_order();
                 }
 #pragma unroll
-                for (int e = tid * 4; e < VB * DKP; e += 2048) {
+                for (int e = tid * 4; e < VB * DKP; e += THREADS * 4) {
                     const int at = s.v.S0.off(e / DKP, e % DKP);
                     z = M::dot4(s.v.S0.e + at, s.v.dS.e + at, z);
                 }
             }
             __syncthreads();
-            // (K Q^T)[j][i] in the first half's waves, (K K^T)[j][i] in the second's
-            f32x4 kx[4];
-#pragma unroll
-            for (int t = 0; t < 4; ++t)
-                kx[t] = f32x4{0, 0, 0, 0};
-            const Tile<El, L, DKP>& other = half ? s.k : s.q;
-#pragma unroll
-            for (int u = 0; u < UK; ++u) {
-                const Frag b = M::rows(other, wave, u, tid);
-                Frag ak[4];
-#pragma unroll
-                for (int t = 0; t < 4; ++t)
-                    ak[t] = M::rows(s.k, t, u, tid);
-                in_order();
-#pragma unroll
-                for (int t = 0; t < 4; ++t)
-                    if (M::reaches(t, wave))
-                        kx[t] = M::mma(ak[t], b, kx[t]);
-                in_order();
-            }
-            // E^T (first half) or F^T in place of the products; sums over i and over j of E q.k, F k.k
+            // (K Q^T)[j][i] for E, (K K^T)[j][i] for F; then E^T, F^T in place of the products r dO^T, r dV^T, and the
+            // sums over i and over j of E q.k, F k.k
             const double Gi = s.G[i];
-            float row = 0.0f, diag = 0.0f;
 #pragma unroll
-            for (int t = 0; t < 4; ++t) {
-                f32x4 y = {0, 0, 0, 0}, w = {0, 0, 0, 0};
-                if (M::reaches(t, wave)) {
+            for (int n = 0; n < NH; ++n) {
+                const int second = NH == 2 ? n : half;
+                f32x4 kx[4];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const int j = M::at(t, g) + e;
-                        const float m = j <= i - half ? fast_exp((float)(Gi - s.G[j])) : 0.0f;
-                        const float f = (half ? -m : a.scale * m) * dX[t][e], b = s.beta[j], both = f * kx[t][e];
-                        y[e] = j < i ? both : 0.0f;
-                        diag += j == i ? both : 0.0f;  // (one lane of the four that have step i)
-                        row = __builtin_fmaf(b, y[e], row);
-                        w[e] = f * b;
-                    }
+                for (int t = 0; t < 4; ++t)
+                    kx[t] = f32x4{0, 0, 0, 0};
+                const Tile<El, L, DKP>& other = second ? s.k : s.q;
 #pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        y[e] = sum16(y[e]);
+                for (int u = 0; u < UK; ++u) {
+                    const Frag b = M::rows(other, wave, u, tid);
+                    Frag ak[4];
+#pragma unroll
+                    for (int t = 0; t < 4; ++t)
+                        ak[t] = M::rows(s.k, t, u, tid);
+                    in_order();
+#pragma unroll
+                    for (int t = 0; t < 4; ++t)
+                        if (M::reaches(t, wave))
+                            kx[t] = M::mma(ak[t], b, kx[t]);
+                    in_order();
                 }
-                if (col == 0)
-                    *(f32x4*)(s.sum[wave8] + M::at(t, g)) = y;
-                put4<BF>(s.EF[half].e + s.EF[half].off(i, M::at(t, g)), w);
-                in_order();
+                float row = 0.0f, diag = 0.0f;
+#pragma unroll
+                for (int t = 0; t < 4; ++t) {
+                    f32x4 y = {0, 0, 0, 0}, w = {0, 0, 0, 0};
+                    if (M::reaches(t, wave)) {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const int j = M::at(t, g) + e;
+                            const float m = j <= i - second ? fast_exp((float)(Gi - s.G[j])) : 0.0f;
+                            const float f = (second ? -m : a.scale * m) * dX[n][t][e], b = s.beta[j], both = f * kx[t][e];
+                            y[e] = j < i ? both : 0.0f;
+                            diag += j == i ? both : 0.0f;  // (one lane of the four that have step i)
+                            row = __builtin_fmaf(b, y[e], row);
+                            w[e] = f * b;
+                        }
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            y[e] = sum16(y[e]);
+                    }
+                    if (col == 0)
+                        *(f32x4*)(s.sum[4 * second + wave] + M::at(t, g)) = y;
+                    put4<BF>(s.EF[second].e + s.EF[second].off(i, M::at(t, g)), w);
+                    in_order();
+                }
+#pragma unroll
+                for (int o = 16; o < 64; o <<= 1) {
+                    row += __shfl_xor(row, o);
+                    diag += __shfl_xor(diag, o);
+                }
+                if (lane < 16) {
+                    s.row[second][i] = row;
+                    if (second == 0)
+                        s.diag[i] = diag;
+                }
             }
             // products with the states, and what the gates take of them
             float ra = 0.0f, rx = 0.0f;
             const float eG = s.eG[i], to_end = s.to_end[i], bi = s.beta[i];
 #pragma unroll
             for (int t = 0; t < TH; ++t) {
-                const int at = Tile<El, L, DKP>::off(i, M::at(half * TH + t, g));
+                const int at = Tile<El, L, DKP>::off(i, M::at(dt + t, g));
                 const El *pk = s.k.e + at, *pq = s.q.e + at;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
@@ -1083,17 +1109,14 @@ __global__ __launch_bounds__(512) void delta_grads(DeltaArgs a)
             }
 #pragma unroll
             for (int o = 16; o < 64; o <<= 1) {
-                row += __shfl_xor(row, o);
-                diag += __shfl_xor(diag, o);
                 ra += __shfl_xor(ra, o);
                 rx += __shfl_xor(rx, o);
             }
             if (lane < 16) {
-                s.row[half][i] = row;
                 s.a[half][i] = ra;
                 s.x[half][i] = rx;
-                if (half == 0)
-                    s.diag[i] = diag;
+                if (NH == 2)
+                    s.a[1][i] = s.x[1][i] = 0.0f;
             }
 #pragma unroll
             for (int o = 1; o < 64; o <<= 1)
@@ -1109,8 +1132,8 @@ __global__ __launch_bounds__(512) void delta_grads(DeltaArgs a)
                 Frag ak[TH], aq[TH];
 #pragma unroll
                 for (int t = 0; t < TH; ++t) {
-                    ak[t] = M::cols(s.k, half * TH + t, u, tid);
-                    aq[t] = M::cols(s.q, half * TH + t, u, tid);
+                    ak[t] = M::cols(s.k, dt + t, u, tid);
+                    aq[t] = M::cols(s.q, dt + t, u, tid);
                 }
                 in_order();
 #pragma unroll
@@ -1125,10 +1148,11 @@ __global__ __launch_bounds__(512) void delta_grads(DeltaArgs a)
             if (wave8 == 0) {
                 float colsum = 0.0f, zs = 0.0f;
 #pragma unroll
-                for (int w = 0; w < 8; ++w) {
+                for (int w = 0; w < 8; ++w)
                     colsum += s.sum[w][lane];
+#pragma unroll
+                for (int w = 0; w < THREADS / 64; ++w)
                     zs += s.z[w];
-                }
                 const float x = s.x[0][lane] + s.x[1][lane], b = s.beta[lane];
                 // sum_{i >= t} of what step i reads, less what it wrote: pairs with both ends behind t cancel (a
                 // step's own pair is left out of both, so a lone step's gradient is 0)
@@ -1158,7 +1182,7 @@ __global__ __launch_bounds__(512) void delta_grads(DeltaArgs a)
         T* pk = (T*)a.grad_k + at;
 #pragma unroll
         for (int t = 0; t < TH; ++t) {
-            const int d = M::at(half * TH + t, g);
+            const int d = M::at(dt + t, g);
             if (i >= live)
                 dq[t] = dk[t] = f32x4{0, 0, 0, 0};
             if (VEC) {  // (Dk is a multiple of 4 and the rows are aligned to them)
@@ -1214,9 +1238,9 @@ template <typename D, bool BF, int DKP, bool VEC> hipError_t backward(const Delt
         return err;
     const dim3 grid((unsigned)((int64_t)a.N * a.Hk * a.nc));
     if (a.Hk == a.Hv)
-        delta_grads<D, BF, DKP, VEC, true><<<grid, dim3(512), 0, s>>>(a);
+        delta_grads<D, BF, DKP, VEC, true><<<grid, dim3(GradsShape<BF, true>::THREADS), 0, s>>>(a);
     else
-        delta_grads<D, BF, DKP, VEC, false><<<grid, dim3(512), 0, s>>>(a);
+        delta_grads<D, BF, DKP, VEC, false><<<grid, dim3(GradsShape<BF, false>::THREADS), 0, s>>>(a);
     return hipGetLastError();
 }
 

@@ -179,12 +179,14 @@ template <> struct Mat<true> {
 template <typename El, int ROWS, int COLS> struct Tile {
     static constexpr bool SWIZZLED = sizeof(El) == 2;
     static constexpr int VE = 16 / sizeof(El), PIECES = COLS / VE, LD = SWIZZLED ? COLS : COLS + VE;
-    static_assert(!SWIZZLED || PIECES == 8 || PIECES == 16);
+    static_assert(!SWIZZLED || PIECES == 4 || PIECES == 8 || PIECES == 16);
     alignas(16) El e[ROWS * LD];
 
     // (an operand's rows are 8 a + {0 .. 3} or 8 a + {4 .. 7}, a = 0 .. 3)
     __device__ static constexpr int swizzle(int row)
     {
+        if (PIECES == 4)
+            return (row >> 3) & 3;
         return PIECES == 8 ? ((row >> 1) & 1) << 2 | ((row >> 3) & 3) : (row & 3) << 2 | ((row >> 3) & 3);
     }
     __device__ static constexpr int off(int row, int col)
