@@ -991,36 +991,41 @@ __global__ __launch_bounds__((GradsShape<BF, ONE>::THREADS), 2) void delta_grads
                     const Frag bo = M::rows(s.v.dO, wave, u, tid);
                     const Frag bv = M::rows(s.v.dV, wave, u, tid);
                     const Frag br = M::cols(s.v.r, wave, u, tid);
-                    Frag ar[4], as[TH];
-#pragma unroll
-                    for (int t = 0; t < TH; ++t)
-                        as[t] = M::cols(s.v.S0, dt + t, u, tid);
-#pragma unroll
-                    for (int t = 0; t < 4; ++t)
-                        ar[t] = M::cols(s.v.r, t, u, tid);
-                    in_order();
-#pragma unroll
-                    for (int t = 0; t < TH; ++t) {
-                        qs[t] = M::mma(as[t], bo, qs[t]);
-                        ks[t] = M::mma(as[t], bv, ks[t]);
-                    }
-                    in_order();
-#pragma unroll
-                    for (int t = 0; t < TH; ++t)
-                        as[t] = M::cols(s.v.dS, dt + t, u, tid);
-                    in_order();
+                    // (a half of the keys' rows at a time: their operands and sums fill the registers)
+                    Frag ar[4], as[TH / NH];
 #pragma unroll
                     for (int n = 0; n < NH; ++n) {
+#pragma unroll
+                        for (int t = 0; t < TH / NH; ++t)
+                            as[t] = M::cols(s.v.S0, dt + n * (TH / NH) + t, u, tid);
+                        if (n + 1 == NH)
+#pragma unroll
+                            for (int t = 0; t < 4; ++t)
+                                ar[t] = M::cols(s.v.r, t, u, tid);
+                        in_order();
+#pragma unroll
+                        for (int t = 0; t < TH / NH; ++t) {
+                            qs[n * (TH / NH) + t] = M::mma(as[t], bo, qs[n * (TH / NH) + t]);
+                            ks[n * (TH / NH) + t] = M::mma(as[t], bv, ks[n * (TH / NH) + t]);
+                        }
+                        in_order();
+                    }
+#pragma unroll
+                    for (int n = 0; n < NH; ++n) {
+#pragma unroll
+                        for (int t = 0; t < TH / NH; ++t)
+                            as[t] = M::cols(s.v.dS, dt + n * (TH / NH) + t, u, tid);
+                        in_order();
                         const Frag bx = (NH == 2 ? n : half) ? bv : bo;
 #pragma unroll
                         for (int t = 0; t < 4; ++t)
                             if (M::reaches(t, wave))
                                 dX[n][t] = M::mma(ar[t], bx, dX[n][t]);
-                    }
 #pragma unroll
-                    for (int t = 0; t < TH; ++t)
-                        ws[t] = M::mma(as[t], br, ws[t]);
-                    in_order();
+                        for (int t = 0; t < TH / NH; ++t)
+                            ws[n * (TH / NH) + t] = M::mma(as[t], br, ws[n * (TH / NH) + t]);
+                        in_order();
+                    }
                 }
 #pragma unroll
                 for (int e = tid * 4; e < VB * DKP; e += THREADS * 4) {
