@@ -69,6 +69,23 @@ __device__ __forceinline__ int64_t unit_of(const DeltaArgs& a, int n, int hv, in
     return ((int64_t)n * a.Hv + hv) * a.nc + c;
 }
 
+// Block b of `count` units of `parts` blocks each: its unit and part, such that
+// the parts of one unit, which read the same tiles, run on one XCD (blocks go to
+// the 8 XCDs in turn) and share them in its L2
+__device__ __forceinline__ void unit_and_part(uint32_t b, uint32_t count, uint32_t parts, uint32_t* unit, uint32_t* part)
+{
+    const uint32_t even = count / 8 * 8;
+    if (b < even * parts) {
+        const uint32_t r = b % (8 * parts);
+        *unit = b / (8 * parts) * 8 + r % 8;
+        *part = r / 8;
+    } else {
+        b -= even * parts;
+        *unit = even + b / parts;
+        *part = b % parts;
+    }
+}
+
 // X = (I + A)^-1 of the strictly lower triangle A [L][LF] in LDS, by four
 // waves: the 16x16 diagonal blocks by substitution (a lane has one column of
 // one block), then twice joined, [[X0, 0], [-X1 A10 X0, X1]].  In float
@@ -299,8 +316,10 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(BF && S
     __shared__ Lds s;
     const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, col = lane & 15, g = lane >> 4;
     const int vblocks = (a.dvp + 63) / 64, blocks = STATES ? vblocks + DKP / 64 : vblocks;
-    const int vb = (int)(blockIdx.x % blocks), seg = (int)(blockIdx.x / blocks % a.nseg);
-    const int64_t head = blockIdx.x / blocks / a.nseg;
+    uint32_t walk, part;
+    unit_and_part(blockIdx.x, (uint32_t)a.N * a.Hv * a.nseg, blocks, &walk, &part);
+    const int vb = (int)part, seg = (int)(walk % a.nseg);
+    const int64_t head = walk / a.nseg;
     const bool values = !STATES || vb < vblocks;
     const int n = (int)(head / a.Hv), hv = (int)(head - (int64_t)n * a.Hv), hk = hv / (a.Hv / a.Hk);
     const int v0 = vb * 64, vl = M::at(wave, col >> 2) + (col & 3), v = v0 + vl, cols = min(64, a.Dv - v0);
@@ -668,10 +687,11 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(1, 1)))
     static_assert(NW == 4 && TH >= 3 * L);
     __shared__ Lds s;
     const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, col = lane & 15, g = lane >> 4;
-    const int vblocks = (a.dvp + 16 * NW - 1) / (16 * NW);
-    const int64_t head = blockIdx.x / vblocks;
+    uint32_t walk, vb;
+    unit_and_part(blockIdx.x, (uint32_t)a.N * a.Hv, (a.dvp + 63) / 64, &walk, &vb);
+    const int64_t head = walk;
     const int n = (int)(head / a.Hv), hv = (int)(head - (int64_t)n * a.Hv), hk = hv / (a.Hv / a.Hk);
-    const int v0 = (int)(blockIdx.x % vblocks) * 64, vl = M::at(wave, col >> 2) + (col & 3), v = v0 + vl, cols = min(64, a.Dv - v0);
+    const int v0 = (int)vb * 64, vl = M::at(wave, col >> 2) + (col & 3), v = v0 + vl, cols = min(64, a.Dv - v0);
     const bool mine = v < a.Dv, wide = v < a.dvp;
     const int len = length_of(a, n), chunks = (len + L - 1) / L;
     f32x4 S[TK];
