@@ -62,20 +62,23 @@ inline int delta_elem(int dtype) { return dtype == 1 ? 2 : 4; }
 inline int delta_dkp(int Dk) { return Dk <= 64 ? 64 : 128; }
 
 // Segments of a forward over `blocks` blocks (sequences x value heads x 64
-// columns) and nc chunks.  A block walks its chunks one after the other, 3.4 us
+// columns) and nc chunks.  A block walks its chunks one after the other, 4 us
 // each (bf16, Dk = Dv = 128), and 256 CUs take a block each, so few heads leave
 // most of the chip idle.  With S segments the chunks are walked three times (for
-// the states without and the transitions, then for the outputs), but in S places at once,
-// and the segments' states are joined in order (4 us a segment): worth it from
-// four segments on, of 16 chunks at least.
+// the states without and the transitions at once, then for the outputs), but in
+// S places at once, and the segments' states are joined in order, 6 us a segment:
+// two walks of nc / S chunks against 6 S is least near S^2 = nc.  Worth it from
+// 32 chunks and four segments on (bf16, in one piece -> in segments, us):
+//   8 blocks, 16 chunks in four: 80 -> 76, 32 chunks: 144 -> 102, 128 chunks: 528 -> 171
+//   64 blocks, 16 chunks in four: 85 -> 90, 32 chunks: 151 -> 128, 256 chunks: 1120 -> 682
+//   128 blocks, two segments, 32 chunks: 167 -> 192, 256 chunks: 1238 -> 1322
 inline int delta_segments(int64_t blocks, int64_t nc)
 {
-    if (blocks < 1 || blocks > 64)
+    if (blocks < 1 || blocks > 64 || nc < 32)
         return 1;
-    int64_t s = 256 / blocks;
-    s = s < nc / 16 ? s : nc / 16;
-    if (s < 4)
-        return 1;
+    int64_t s = 4;
+    while ((s + 1) * (s + 1) <= nc && s + 1 <= 256 / blocks)
+        ++s;
     const int64_t each = (nc + s - 1) / s;
     return (int)((nc + each - 1) / each);
 }

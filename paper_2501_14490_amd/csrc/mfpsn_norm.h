@@ -24,14 +24,24 @@ struct NormArgs {
     float* grad_beta;    // nullable
 };
 
-// Blocks of the backward for M rows of C channels and S columns (host; the
-// workspace has 2 C floats for each): one for 4 rows (S = 1) or a tile of 64
-// columns, up to 4 waves for each SIMD, 8 for few channels, whose tiles are
-// short of loads in flight and whose partial sums are small.
-constexpr int kNormMaxBlocks = 2048;
+// Most blocks of the backward for M rows of C channels and S columns (host; the
+// workspace has 2 C floats for each).  A block sums its columns' share of the
+// weights' gradients in registers and writes it once, so fewer blocks save that,
+// the weights' reads and their join, as long as the loads in flight last: wider
+// rows and tiles have more of them a block.  Measured (us; 1024, 512, 256 blocks):
+//   rows    f32 [500000][64]    75, 82 (512), 77;    f32 [64000][512]   82, 75, 88
+//           bf16 [20000][2048]  95, 72, 62
+//   planes  bf16 [3000][12][1936]  121, 141, -;      bf16 [960][64][1936] 171, 155, 157
+//           bf16 [500][256][700]   155, 136, 161;    bf16 [16][1024][4096] 137, 132, 124
+//   planes of one column a lane (S odd)  bf16 [960][64][1935]  191, 214, 217
+constexpr int kNormMaxBlocks = 1024;
 inline int norm_blocks(int64_t M, int64_t C, int64_t S)
 {
-    const int64_t work = S == 1 ? (M + 3) / 4 : (M * S + 63) / 64, most = C <= 256 ? kNormMaxBlocks : kNormMaxBlocks / 2;
+    const int64_t work = S == 1 ? (M + 3) / 4 : (M * S + 63) / 64;
+    const int64_t few = S == 1 ? 64 : 16, some = S == 1 ? 1024 : 256;
+    int64_t most = C <= few ? kNormMaxBlocks : (C <= some ? kNormMaxBlocks / 2 : kNormMaxBlocks / 4);
+    if (S > 1 && S % 2 && most < kNormMaxBlocks)
+        most *= 2;
     return (int)(work < 1 ? 1 : (work < most ? work : most));
 }
 

@@ -19,8 +19,9 @@
 // threads, then over the blocks by a second kernel in double, each in a fixed
 // order, so repeated calls give the same bits.
 //
-// S = 1: the channels are contiguous; a wave (or the block's four waves, for
-// long rows) takes a row, 16 bytes a lane and load where rows are aligned.
+// S = 1: the channels are contiguous; a wave (a part of one for short rows, the
+// block's four for long ones) takes a row, 16 bytes a lane and load where rows
+// are aligned.
 // S > 1: a block takes a tile of neighbouring columns (m, s) and all channels;
 // lanes run over the columns, and the channels are spread over the lanes'
 // rows and the waves.
@@ -71,29 +72,28 @@ template <typename V> __device__ __forceinline__ void again(V& v)
     }
 }
 
-__device__ __forceinline__ float wave_sum(float v)
+// Sum over groups of N neighbouring lanes
+template <int N> __device__ __forceinline__ float lanes_sum(float v)
 {
 #pragma unroll
-    for (int o = 32; o > 0; o >>= 1)
+    for (int o = N / 2; o > 0; o >>= 1)
         v += __shfl_xor(v, o);
     return v;
 }
 
-// Sum over the WPR waves that share a row; `at` alternates between calls so
-// that one barrier a call is enough
-template <int WPR>
+// Sum over the LANES lanes that share a row (8 to 64 or, through LDS, all 256
+// of a block); `at` alternates between calls so that one barrier a call is enough
+template <int LANES>
 __device__ __forceinline__ float row_sum(float v, float (*lds)[4], int& at)
 {
-    v = wave_sum(v);
-    if constexpr (WPR > 1) {
+    v = lanes_sum<(LANES < 64 ? LANES : 64)>(v);
+    if constexpr (LANES > 64) {
+        static_assert(LANES == kT && kT == 256);
         const int w = threadIdx.x >> 6;
         if ((threadIdx.x & 63) == 0)
             lds[at][w] = v;
         __syncthreads();
-        v = lds[at][0];
-#pragma unroll
-        for (int i = 1; i < WPR; ++i)
-            v += lds[at][i];
+        v = (lds[at][0] + lds[at][1]) + (lds[at][2] + lds[at][3]);
         at ^= 1;
     }
     return v;
@@ -124,12 +124,12 @@ __device__ __forceinline__ void load_weights(const float* __restrict__ w, float 
 // ---------------------------------------------------------------------------
 
 // A lane's elements of a row: NV loads of VE neighbours, LANES lanes a row
-template <typename D, int VE, int NV, int WPR>
+template <typename D, int VE, int NV, int LANES>
 __global__ __launch_bounds__(kT) void norm_fwd_rows(NormArgs a)
 {
     using T = typename D::T;
     using V = Vec<T, VE>;
-    constexpr int LANES = 64 * WPR, ROWS = 4 / WPR;
+    constexpr int ROWS = kT / LANES;
     __shared__ float lds[2][4];
     int at = 0;
     const int lane = threadIdx.x % LANES, sub = threadIdx.x / LANES;
@@ -158,7 +158,7 @@ __global__ __launch_bounds__(kT) void norm_fwd_rows(NormArgs a)
                 s += e < C ? f[i][j] : 0.0f;
             }
         }
-        const float mean = row_sum<WPR>(s, lds, at) * inv;
+        const float mean = row_sum<LANES>(s, lds, at) * inv;
         float q = 0.0f;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
@@ -169,7 +169,7 @@ __global__ __launch_bounds__(kT) void norm_fwd_rows(NormArgs a)
                 q += e < C ? f[i][j] * f[i][j] : 0.0f;
             }
         }
-        const float rstd = 1.0f / sqrtf(row_sum<WPR>(q, lds, at) * inv + a.eps);
+        const float rstd = 1.0f / sqrtf(row_sum<LANES>(q, lds, at) * inv + a.eps);
         if (lane == 0 && a.mean) {
             a.mean[m] = mean;
             a.rstd[m] = rstd;
@@ -203,12 +203,12 @@ __global__ __launch_bounds__(kT) void norm_fwd_long(NormArgs a)
         float s = 0.0f, q = 0.0f;
         for (int e = threadIdx.x; e < C; e += kT)
             s += D::get(x[e]);
-        const float mean = row_sum<4>(s, lds, at) * inv;
+        const float mean = row_sum<kT>(s, lds, at) * inv;
         for (int e = threadIdx.x; e < C; e += kT) {
             const float d = D::get(x[e]) - mean;
             q += d * d;
         }
-        const float rstd = 1.0f / sqrtf(row_sum<4>(q, lds, at) * inv + a.eps);
+        const float rstd = 1.0f / sqrtf(row_sum<kT>(q, lds, at) * inv + a.eps);
         if (threadIdx.x == 0 && a.mean) {
             a.mean[m] = mean;
             a.rstd[m] = rstd;
@@ -218,12 +218,12 @@ __global__ __launch_bounds__(kT) void norm_fwd_long(NormArgs a)
     }
 }
 
-template <typename D, int VE, int NV, int WPR>
+template <typename D, int VE, int NV, int LANES>
 __global__ __launch_bounds__(kT) void norm_bwd_rows(NormArgs a)
 {
     using T = typename D::T;
     using V = Vec<T, VE>;
-    constexpr int LANES = 64 * WPR, ROWS = 4 / WPR;
+    constexpr int ROWS = kT / LANES;
     __shared__ float lds[2][4];
     __shared__ float sums[ROWS > 1 ? (ROWS - 1) * LANES : 1];
     int at = 0;
@@ -258,8 +258,8 @@ __global__ __launch_bounds__(kT) void norm_bwd_rows(NormArgs a)
                 sh += al * xh;
             }
         }
-        const float ma = row_sum<WPR>(sa, lds, at) * inv;
-        const float mh = row_sum<WPR>(sh, lds, at) * inv;
+        const float ma = row_sum<LANES>(sa, lds, at) * inv;
+        const float mh = row_sum<LANES>(sh, lds, at) * inv;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int e = (i * LANES + lane) * VE;
@@ -321,8 +321,8 @@ __global__ __launch_bounds__(kT) void norm_bwd_long(NormArgs a)
             sa += al;
             sh += al * (D::get(x[e]) - mean) * rstd;
         }
-        const float ma = row_sum<4>(sa, lds, at) * inv;
-        const float mh = row_sum<4>(sh, lds, at) * inv;
+        const float ma = row_sum<kT>(sa, lds, at) * inv;
+        const float mh = row_sum<kT>(sh, lds, at) * inv;
         for (int e = threadIdx.x; e < C; e += kT) {
             const float al = D::get(gy[e]) * (a.gamma ? a.gamma[e] : 1.0f);
             gx[e] = D::put(rstd * (al - ma - (D::get(x[e]) - mean) * rstd * mh));
@@ -623,8 +623,8 @@ __global__ __launch_bounds__(kT) void norm_bwd_planes_weights(NormArgs a)
         gg += g * ((D::get(((const T*)a.x)[i]) - a.mean[j]) * a.rstd[j]);
         gb += g;
     }
-    gg = wave_sum(gg);
-    gb = wave_sum(gb);
+    gg = lanes_sum<64>(gg);
+    gb = lanes_sum<64>(gb);
     if (lane == 0) {
         float* __restrict__ part = a.part + (int64_t)blockIdx.y * 2 * C;
         part[c] = gg;
@@ -669,43 +669,53 @@ __global__ __launch_bounds__(1024) void norm_weights_kernel(const float* __restr
 
 hipError_t last() { return hipGetLastError(); }
 
-template <typename D, int VE, int NV, int WPR>
-hipError_t rows(const NormArgs& a, bool bwd, int blocks, hipStream_t s)
+// used: blocks of the launch, `most` or as many as have rows
+template <typename D, int VE, int NV, int LANES>
+hipError_t rows(const NormArgs& a, bool bwd, int most, hipStream_t s, int* used)
 {
+    constexpr int ROWS = kT / LANES;
+    const int64_t need = (a.M + ROWS - 1) / ROWS;
+    *used = need < 1 ? 1 : (int)(need < most ? need : most);
     if (bwd)
-        norm_bwd_rows<D, VE, NV, WPR><<<dim3(blocks), dim3(kT), 0, s>>>(a);
+        norm_bwd_rows<D, VE, NV, LANES><<<dim3(*used), dim3(kT), 0, s>>>(a);
     else
-        norm_fwd_rows<D, VE, NV, WPR><<<dim3(blocks), dim3(kT), 0, s>>>(a);
+        norm_fwd_rows<D, VE, NV, LANES><<<dim3(*used), dim3(kT), 0, s>>>(a);
     return last();
 }
 
-// the smallest of the kernels whose registers hold a row: a wave of up to
-// 32 elements a lane, else four waves; false: none does
+// the smallest of the kernels whose registers hold a row: a part of a wave or
+// a whole one of up to 32 elements a lane, else four waves; false: none does.
+// (f32 [500000][64]: 46 us by quarters of a wave, 96 by waves of 48 idle lanes)
 template <typename D, int VE>
-bool launch_rows(const NormArgs& a, bool bwd, int blocks, hipStream_t s, hipError_t* err)
+bool launch_rows(const NormArgs& a, bool bwd, int most, hipStream_t s, int* used, hipError_t* err)
 {
     const int64_t per = ((int64_t)a.C + VE - 1) / VE;  // loads of a row
     constexpr int MAX = 32 / VE < 8 ? 32 / VE : 8;
-    const auto fits = [&](int nv, int wpr) { return per <= (int64_t)nv * 64 * wpr; };
-    if (fits(1, 1)) *err = rows<D, VE, 1, 1>(a, bwd, blocks, s);
-    else if (fits(2, 1)) *err = rows<D, VE, 2, 1>(a, bwd, blocks, s);
-    else if (fits(4, 1)) *err = rows<D, VE, 4, 1>(a, bwd, blocks, s);
-    else if (MAX == 8 && fits(8, 1)) *err = rows<D, VE, MAX, 1>(a, bwd, blocks, s);
-    else if (fits(4, 4)) *err = rows<D, VE, 4, 4>(a, bwd, blocks, s);
-    else if (MAX == 8 && fits(8, 4)) *err = rows<D, VE, MAX, 4>(a, bwd, blocks, s);
+    const auto fits = [&](int nv, int lanes) { return per <= (int64_t)nv * lanes; };
+    if (fits(1, 8)) *err = rows<D, VE, 1, 8>(a, bwd, most, s, used);
+    else if (fits(1, 16)) *err = rows<D, VE, 1, 16>(a, bwd, most, s, used);
+    else if (fits(1, 32)) *err = rows<D, VE, 1, 32>(a, bwd, most, s, used);
+    else if (fits(1, 64)) *err = rows<D, VE, 1, 64>(a, bwd, most, s, used);
+    else if (fits(2, 64)) *err = rows<D, VE, 2, 64>(a, bwd, most, s, used);
+    else if (fits(4, 64)) *err = rows<D, VE, 4, 64>(a, bwd, most, s, used);
+    else if (MAX == 8 && fits(8, 64)) *err = rows<D, VE, MAX, 64>(a, bwd, most, s, used);
+    else if (fits(4, kT)) *err = rows<D, VE, 4, kT>(a, bwd, most, s, used);
+    else if (MAX == 8 && fits(8, kT)) *err = rows<D, VE, MAX, kT>(a, bwd, most, s, used);
     else return false;
     return true;
 }
 
 // The widest tile whose channels the registers of a block hold.  Tiles of 512
 // bytes a channel (64 lanes) rather than 128 where there are few channels: rows
-// that start at no cache line share two lines with the neighbouring tiles.
-template <typename D, int VE> hipError_t launch_planes(const NormArgs& a, bool bwd, int most, hipStream_t s, bool* cached)
+// that start at no cache line share two lines with the neighbouring tiles (bf16
+// [960][64][1936], forward and backward: 113 and 180 us against 202 and 299).
+template <typename D, int VE> hipError_t launch_planes(const NormArgs& a, bool bwd, int most, hipStream_t s, int* used, bool* cached)
 {
     constexpr int HALF = VE > 1 ? VE / 2 : 1;
-    const auto grid = [&](int width) {
-        const int64_t tiles = (a.M * a.S + width - 1) / width;
-        return dim3((unsigned)(bwd || tiles > most ? most : (tiles < 1 ? 1 : tiles)));
+    const auto grid = [&](int width) {  // as many blocks as have tiles, and as many tiles each where there are more
+        const int64_t tiles = (a.M * a.S + width - 1) / width, each = (tiles + most - 1) / most;
+        const int64_t need = tiles > most ? ((tiles + each - 1) / each + 7) / 8 * 8 : tiles;  // (a multiple of 8: first_tile)
+        return dim3(*used = (int)(need < 1 ? 1 : (need < most ? need : most)));
     };
     *cached = true;
 #define MFPSN_PLANES(VEC, LX, NW, NP, CACHED)                                                          \
@@ -740,6 +750,14 @@ template <typename D, int VE> hipError_t launch_planes(const NormArgs& a, bool b
 #undef MFPSN_PLANES
 }
 
+// Most blocks of the forward.  A block reads its lanes' weights once, so a few
+// rows each pay for them; fewer blocks leave loads in flight unused.  (us; 2048,
+// 1024, 512, 256 blocks) f32 [64000][512]: 46, 44, 50, 84; f32 [500000][64]: 46,
+// 45, 70, 121; bf16 [20000][2048]: 69, 46, 41, 47.  Tiles: (2048, 4096, 8192,
+// 16384) bf16 [960][64][1936]: 114, 105, 106, 106; bf16 [500][256][700]: 95, 91,
+// 113, 113; one column a lane, bf16 [960][64][1935]: 130, 139, 125, 113.
+constexpr int kFwdRows = 1024, kFwdPlanes = 4096;
+
 template <typename D> hipError_t run(const NormArgs& a, bool bwd, hipStream_t s)
 {
     constexpr int VE = 16 / sizeof(typename D::T);
@@ -747,15 +765,16 @@ template <typename D> hipError_t run(const NormArgs& a, bool bwd, hipStream_t s)
     const auto al = [&](size_t n) {
         return (uintptr_t)a.x % n == 0 && (uintptr_t)a.out % n == 0 && (!bwd || (uintptr_t)a.gy % n == 0);
     };
-    bool whole = true;  // the kernel sums the weights' gradients too
+    bool whole = true;  // the kernel sums the weights' gradients too, in `used` partial sums
+    int used = blocks;
     hipError_t err = hipSuccess;
     if (a.S == 1) {
-        const int grid = bwd ? blocks : (int)((a.M + 3) / 4 < 2048 ? (a.M + 3) / 4 : 2048);
-        const bool done = a.C % VE == 0 && al(16) ? launch_rows<D, VE>(a, bwd, grid, s, &err)
-                                                  : launch_rows<D, 1>(a, bwd, grid, s, &err);
+        const int most = bwd ? blocks : (a.C <= 1024 ? kFwdRows : kFwdRows / 2);
+        const bool done = a.C % VE == 0 && al(16) ? launch_rows<D, VE>(a, bwd, most, s, &used, &err)
+                                                  : launch_rows<D, 1>(a, bwd, most, s, &used, &err);
         if (!done) {
             whole = false;
-            const int g = (int)(a.M < (1 << 20) ? a.M : (1 << 20));
+            const int g = (int)(a.M < 1 ? 1 : (a.M < (1 << 20) ? a.M : (1 << 20)));
             if (bwd)
                 norm_bwd_long<D><<<dim3(g), dim3(kT), 0, s>>>(a);
             else
@@ -763,12 +782,13 @@ template <typename D> hipError_t run(const NormArgs& a, bool bwd, hipStream_t s)
             err = last();
         }
     } else {
-        err = a.S % (VE / 2) == 0 && al(8) ? launch_planes<D, VE / 2>(a, bwd, bwd ? blocks : kNormMaxBlocks, s, &whole)
-                                           : launch_planes<D, 1>(a, bwd, bwd ? blocks : kNormMaxBlocks, s, &whole);
+        err = a.S % (VE / 2) == 0 && al(8) ? launch_planes<D, VE / 2>(a, bwd, bwd ? blocks : kFwdPlanes, s, &used, &whole)
+                                           : launch_planes<D, 1>(a, bwd, bwd ? blocks : 4 * kFwdPlanes, s, &used, &whole);
     }
     if (err != hipSuccess || !bwd || !a.part)
         return err;
     if (!whole) {
+        used = blocks;
         if (a.S == 1)
             norm_bwd_long_weights<D><<<dim3((a.C + kT - 1) / kT, blocks), dim3(kT), 0, s>>>(a);
         else
@@ -776,7 +796,7 @@ template <typename D> hipError_t run(const NormArgs& a, bool bwd, hipStream_t s)
         if ((err = last()) != hipSuccess)
             return err;
     }
-    norm_weights_kernel<<<dim3((unsigned)((2 * (int64_t)a.C + 15) / 16)), dim3(1024), 0, s>>>(a.part, blocks, a.C, a.grad_gamma,
+    norm_weights_kernel<<<dim3((unsigned)((2 * (int64_t)a.C + 15) / 16)), dim3(1024), 0, s>>>(a.part, used, a.C, a.grad_gamma,
                                                                                         a.grad_beta);
     return last();
 }
