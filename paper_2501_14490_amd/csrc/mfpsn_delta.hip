@@ -147,7 +147,13 @@ __device__ void unit_lower_inverse(const float* A, float* X)
     __syncthreads();
 }
 
-// X, P and the gates of a chunk, for the value heads of one key head
+// X, P and the gates of a chunk, for the value heads of one key head, so that
+// K K^T and K Q^T are computed once for heads that share their keys.  Four blocks
+// a CU: a block's time is a chain of latencies (loads, the products, the
+// substitution's 16 dependent rows, the joins), not its 2 MFLOP; other blocks fill
+// it.  8 x 16 heads of 2048 steps, bf16, Dk = 128: 78 us for 4096 chunks, 270 MB
+// moved, of which X in three parts is 100.  P is rounded once to 16 bits: it makes
+// outputs only, which are rounded likewise, no state.
 template <bool BF, int DKP> struct PrepLds {
     using El = typename Mat<BF>::El;
     union {
@@ -276,6 +282,10 @@ __global__ __launch_bounds__(256, 4) void delta_prep(DeltaArgs a)
 // a SIMD (the state, the operands of the next products and the next tiles
 // take more than half of the registers), so nothing but the order of its own
 // instructions hides a wave's latencies: operands are read a group ahead.
+// Bound by that chain: 256 blocks of 32 chunks (8 x 16 heads of 2048 steps, 128 x
+// 128, bf16) take 194 us, 6 us a chunk, where the 176 matrix instructions of a wave
+// (the products with the state and X in three parts, see below) need 1.2 at their
+// peak rate.  Two waves a SIMD do not fit: 225 registers spill.
 template <bool BF, int DKP, bool STATES> struct ScanLds {
     using El = typename Mat<BF>::El;
     Tile<El, L, DKP> k, q;
@@ -587,7 +597,8 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(BF && S
 
 // The states before the segments of a head, in order: S <- T S + local, in float.
 // A wave has 16 columns, as in the scan; T comes through LDS, the next segment's
-// in four parts while this one's is multiplied with.
+// in four parts while this one's is multiplied with.  A chain too: 6 us a segment
+// (16 heads, 128 x 128, 8 segments: 49 us).
 template <int DKP> __global__ __launch_bounds__(256) void delta_join(DeltaArgs a)
 {
     using M = Mat<false>;
@@ -665,7 +676,12 @@ template <int DKP> __global__ __launch_bounds__(256) void delta_join(DeltaArgs a
 }
 
 // The chunks in reverse, in the same manner: the gradient of the state, the
-// values' gradient
+// values' gradient.  The state's gradient is held in float; as an operand it is
+// rounded once to 16 bits, like the residuals' gradients: what comes of them is
+// stored in 16 bits or (E, F, dS in delta_grads) multiplied in 16 bits.  In two
+// parts each the values' gradient was off by 2.2e-3 of its norm in place of
+// 3.6e-3 (1.7e-3: its own rounding), for 51 of 137 us more (8 x 16 heads of 2048
+// steps, 128 x 128; 4.3 us a chunk, a chain of latencies as in the scan).
 template <bool BF, int DKP> struct RscanLds {
     using El = typename Mat<BF>::El;
     Tile<El, L, DKP> k, q;
@@ -903,7 +919,11 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(1, 1)))
 // so that two blocks share a CU and one computes while the other waits for its
 // reads.  Otherwise the sums over the heads need registers besides, and float
 // tiles the LDS: eight waves, waves w and w + 4 with the same steps, each with
-// half of the keys' rows and one of E and F.
+// half of the keys' rows and one of E and F.  8 x 16 heads of 2048 steps, 128 x
+// 128, bf16: 232 us for 4096 chunks, 0.74 GB moved (3.2 TB/s; the states before and
+// their gradients behind the chunks are 0.27 of it) and 60 GFLOP.  Operands are
+// rounded once to 16 bits (r, S0 and dS were stored so); E and F in two parts cost
+// 10 us more and took grad_q from 2.9e-3 to 2.6e-3 of its norm.
 template <bool BF, int DKP, int VB> struct GradsLds {
     using El = typename Mat<BF>::El;
     Tile<El, L, DKP> k, q;

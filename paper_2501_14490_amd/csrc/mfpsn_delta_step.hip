@@ -3,7 +3,9 @@
 // for a single arriving step (serving) and for sequences too short for the
 // chunked form to pay.  The state (float [N][Hv][Dk][Dv]) is read once, kept in
 // registers over the steps and written once: a single step is bound by those
-// two passes over HBM.
+// two passes over HBM (128 streams of 16 heads, 128 x 128: 52 us, 5.2 TB/s, what
+// a copy reaches; one stream of 4 heads: 4.8 us, the latency of one load, one
+// reduction and one store behind a launch).  All in float; o is rounded once.
 //
 // A block of 256 threads has 32 columns of one head's state: 8 lanes of 4
 // neighbouring columns (128 bytes of a row) by 32 groups of rows, Dk/32 rows a

@@ -730,6 +730,7 @@ class LayerNormFunction(torch.autograd.Function):
         return y
 
     @staticmethod
+    @torch.autograd.function.once_differentiable
     def backward(ctx, grad_y):
         xc, gc, mean, rstd = ctx.saved_tensors
         gy = grad_y.to(xc.dtype).contiguous()
@@ -752,7 +753,17 @@ def make_delta_desc(qk_shape, v_shape, dtype="f32", scale=None) -> MfpsnDeltaDes
     if (T, N) != (Tv, Nv):
         raise ValueError(f"q and k {tuple(qk_shape)} and v {tuple(v_shape)} differ in steps or sequences")
     dt = DTYPES[dtype] if isinstance(dtype, str) else int(dtype)
-    return MfpsnDeltaDesc(T, N, Hk, Hv, Dk, Dv, dt, float(Dk) ** -0.5 if scale is None else float(scale), 0, 0, 0)
+    return MfpsnDeltaDesc(T, N, Hk, Hv, Dk, Dv, dt, max(Dk, 1) ** -0.5 if scale is None else float(scale), 0, 0, 0)
+
+
+def _row_stride(t):
+    """Elements between the rows (t, n) of a [T, N, H, D] tensor, None unless its rows [H, D] are dense and at equal
+    distances."""
+    T, N, H, D = t.shape
+    row = t.stride(1) if N > 1 else t.stride(0)
+    if (D > 1 and t.stride(3) != 1) or (H > 1 and t.stride(2) != D) or (T > 1 and t.stride(0) != N * row) or row < H * D:
+        return None
+    return row
 
 
 def _delta_row(t, dtype, device, shape, name):
@@ -766,9 +777,8 @@ def _delta_row(t, dtype, device, shape, name):
         raise ValueError(f"{name} must be on {device}, got {t.device}")
     if tuple(t.shape) != tuple(shape):
         raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
-    T, N, H, D = shape
-    row = t.stride(1) if N > 1 else t.stride(0)
-    if (D > 1 and t.stride(3) != 1) or (H > 1 and t.stride(2) != D) or (T > 1 and t.stride(0) != N * row) or row < H * D:
+    row = _row_stride(t)
+    if row is None:
         raise ValueError(f"{name} of strides {t.stride()} must have dense rows [H, D] at equal distances")
     return row
 
@@ -889,11 +899,13 @@ class DeltaFunction(torch.autograd.Function):
     """o, state_out = gated delta rule of q, k [T, N, Hk, Dk], v [T, N, Hv, Dv],
     g, beta [T, N, Hv] (float32 or bfloat16, one type for all), scale (None:
     1/sqrt(Dk)), state (float [N, Hv, Dk, Dv] or None) and lengths (int32 [N] or
-    None).  Gradients of all of them but scale and lengths."""
+    None), of any strides (q, k, v are copied unless their rows [H, D] are dense
+    and at equal distances).  Gradients of all of them but scale and lengths."""
 
     @staticmethod
     def forward(ctx, q, k, v, g, beta, scale=None, state=None, lengths=None):
-        ins = [t.detach() for t in (q, k, v)] + [t.detach().contiguous() for t in (g, beta)]
+        ins = [t.detach() if t.dim() != 4 or _row_stride(t) is not None else t.detach().contiguous() for t in (q, k, v)]
+        ins += [t.detach().contiguous() for t in (g, beta)]
         st = state.detach().float().contiguous() if state is not None else None
         desc = make_delta_desc(q.shape, v.shape, _float_dtype(v, "v"), scale)
         o, out, saved = delta_forward(desc, *ins, lengths=lengths, state=st, want_state=True, want_saved=True)
@@ -904,6 +916,7 @@ class DeltaFunction(torch.autograd.Function):
         return o, out
 
     @staticmethod
+    @torch.autograd.function.once_differentiable
     def backward(ctx, grad_o, grad_state):
         q, k, v, g, beta, saved, lengths = ctx.saved_tensors
         if grad_o is None and grad_state is None:

@@ -130,7 +130,8 @@ def test_long_sequence_and_slow_decay(dtype):
 # segment, sequences that end before most segments, keys and values of one and of several tiles, states in and out
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("T,N,Hk,Hv,Dk,Dv,lengths", [(4200, 1, 1, 1, 16, 24, None), (5000, 3, 1, 2, 20, 70, [5000, 130, 0]),
-                                                     (4161, 1, 1, 2, 128, 16, None)])
+                                                     (4161, 1, 1, 2, 128, 16, None), (2049, 2, 2, 2, 40, 33, [2049, 700]),
+                                                     (1985, 4, 8, 8, 16, 70, None)])
 def test_segments_of_a_long_sequence(T, N, Hk, Hv, Dk, Dv, lengths, dtype):
     c = make(T, N, Hk, Hv, Dk, Dv, dtype, seed=T, lengths=lengths, rate=0.003)
     if lengths:
@@ -337,6 +338,47 @@ def test_graph_replays():
         for graph, want, got, _ in graphs:
             for i, (a, b) in enumerate(zip(want, got)):
                 assert torch.equal(a, b), i
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_autograd_of_other_strides_and_broadcast_inputs(dtype):
+    """Batch-first and broadcast inputs give the bits of their dense copies, and a broadcast input the sum of them."""
+    c = make(70, 3, 2, 4, 24, 40, dtype, seed=21)
+    go = dev(c["grad_o"])
+    batch_first = [dev(c[n]).transpose(0, 1).contiguous().requires_grad_() for n in NAMES]
+    o, _ = mfpsn.DeltaFunction.apply(*[t.transpose(0, 1) for t in batch_first], c["scale"])
+    o.backward(go)
+    dense = [dev(c[n]).requires_grad_() for n in NAMES]
+    want, _ = mfpsn.DeltaFunction.apply(*dense, c["scale"])
+    want.backward(go)
+    assert torch.equal(o, want)
+    for x, y in zip(batch_first, dense):
+        assert torch.equal(x.grad, y.grad.transpose(0, 1))
+    k = dev(c["k"])[:, :, :1].detach().requires_grad_()
+    beta = dev(c["beta"])[:, :1, :1].detach().requires_grad_()
+    ins = [dense[0].detach(), k.expand(70, 3, 2, 24), dense[2].detach(), dense[3].detach(), beta.expand(70, 3, 4)]
+    mfpsn.DeltaFunction.apply(*ins, c["scale"])[0].backward(go)
+    whole = [t.detach().clone().requires_grad_() for t in ins]
+    mfpsn.DeltaFunction.apply(*whole, c["scale"])[0].backward(go)
+    assert torch.equal(k.grad, whole[1].grad.sum(2, keepdim=True))
+    # (torch sums the two axes in an order of its own: 11 additions of the type's half step)
+    near_sum = whole[4].grad.double().sum((1, 2), keepdim=True)
+    step = 11 * torch.finfo(beta.dtype).eps / 2 * whole[4].grad.double().abs().sum((1, 2), keepdim=True) + 1e-30
+    assert ((beta.grad.double() - near_sum).abs() <= step).all()
+
+
+def test_second_derivatives_are_refused():
+    c = make(20, 1, 1, 1, 16, 16, "f32", seed=3)
+    leaves = [dev(c[n]).requires_grad_() for n in NAMES]
+    o, _ = mfpsn.DeltaFunction.apply(*leaves, c["scale"])
+    (first,) = torch.autograd.grad((o * o).sum(), leaves[:1], create_graph=True)
+    with pytest.raises(RuntimeError):
+        first.sum().backward()
+    x = torch.randn(4, 8, 1, device=DEV, requires_grad=True)
+    y = mfpsn.LayerNormFunction.apply(x, None, None, 1e-5, 1)
+    (first,) = torch.autograd.grad((y * y).sum(), x, create_graph=True)
+    with pytest.raises(RuntimeError):
+        first.sum().backward()
 
 
 def test_autograd_and_differences():

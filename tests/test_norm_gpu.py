@@ -6,7 +6,7 @@ elements, at most max(32, C/16), then at most 10 joins of lanes and waves):
   xh          off by rstd times that, and (n/2 + 6) e relative (the variance's sum enters by its square root)
   y           gamma xh + beta: two roundings more, and the storage type's half step
   grad_x      r (a - mean a - xh mean(a xh)): the errors of its three terms, each sum n + 4 roundings
-  weights     sums of M S terms, chained at most M S / 1024 + 80 long
+  weights     sums of M S terms, chained at most M S / 1024 + 80 long (at the sizes below)
 """
 import numpy as np
 import pytest
@@ -95,6 +95,8 @@ def test_planes(M, C, S, dtype):
 def test_many_rows_for_each_block(dtype):
     check(20000, 24, 1, dtype)  # more rows than the blocks of the backward take at once
     check(3, 8, 40000, dtype)
+    check(40, 8, 7001, dtype)
+    check(3, 20, 100000, dtype)
 
 
 @pytest.mark.parametrize("S", [1, 6])
@@ -138,6 +140,22 @@ def test_a_row_that_is_not_finite_spoils_no_other(S):
     keep = ~bad[:, None, :].expand(6, 130, S).to(DEV)
     assert torch.equal(got[keep], good[keep])
     assert torch.isnan(got[2, :, 0]).all() and torch.isnan(got[4, 0, 0])
+
+
+# rows of every part of a wave, whole and not, one more and one fewer than fill the blocks' parts
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("M,C", [(1, 8), (31, 24), (33, 32), (1025, 56), (65, 72), (15, 120), (17, 128), (255, 136), (7, 248), (9, 16),
+                                 (2049, 9), (40000, 17), (3, 33)])
+def test_short_rows(M, C, dtype):
+    check(M, C, 1, dtype, seed=M + C)
+
+
+def test_no_rows_of_many_channels():
+    C = 30000  # (more than a block's registers hold)
+    x, gamma = torch.empty((0, C), device=DEV), torch.ones(C, device=DEV)
+    y, mean, rstd = mfpsn.layer_norm_forward(x, gamma, gamma, axis=1, want_stats=True)
+    gx, gg, gb = mfpsn.layer_norm_backward(x, gamma, mean, rstd, y, axis=1)
+    assert gx.shape == x.shape and not gg.any() and not gb.any() and gg.shape == gb.shape == (C,)
 
 
 def test_empty_tensors_and_missing_weights():
