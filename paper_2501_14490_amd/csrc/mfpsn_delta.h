@@ -37,6 +37,7 @@ struct DeltaArgs {
     // long sequences of few heads: cut into segments (delta_segments)
     int32_t nseg, seg_chunks;     // 1 and nc where there is one
     float* local;                 // [head][nseg][dkp][64 vblocks + dkp]: a segment's state from zeros, its transition
+                                  // (the last: neither; the first: its state from state_in)
     float* start;                 // [head][nseg][dkp][64 vblocks]: the state before each segment
     // backward
     const void* grad_o;
@@ -64,20 +65,23 @@ inline int delta_dkp(int Dk) { return Dk <= 64 ? 64 : 128; }
 // Segments of a forward over `blocks` blocks (sequences x value heads x 64
 // columns) and nc chunks.  A block walks its chunks one after the other, 4 us
 // each (bf16, Dk = Dv = 128), and 256 CUs take a block each, so few heads leave
-// most of the chip idle.  With S segments the chunks are walked three times (for
-// the states without and the transitions at once, then for the outputs), but in
-// S places at once, and the segments' states are joined in order, 6 us a segment:
-// two walks of nc / S chunks against 6 S is least near S^2 = nc.  Worth it from
-// 32 chunks and four segments on (bf16, in one piece -> in segments, us):
-//   8 blocks, 16 chunks in four: 80 -> 76, 32 chunks: 144 -> 102, 128 chunks: 528 -> 171
-//   64 blocks, 16 chunks in four: 85 -> 90, 32 chunks: 151 -> 128, 256 chunks: 1120 -> 682
-//   128 blocks, two segments, 32 chunks: 167 -> 192, 256 chunks: 1238 -> 1322
+// most of the chip idle.  With S segments the chunks are walked twice, for the
+// states (and the transitions at once, of all but the first and last segment) and
+// for the outputs, but in S places at once, and the segments' states are joined
+// in order, 4 us a segment: two walks of nc / S chunks against 4 S is least near
+// S^2 = 2 nc.  The fewer segments the CUs take, the longer the sequence that they
+// pay for (bf16, in one piece -> in segments, us):
+//   8 blocks, 16 chunks: 80 -> 68, 32 chunks: 144 -> 83, 128 chunks: 528 -> 138
+//   64 blocks (4), 16 chunks: 85 -> 85, 32 chunks: 151 -> 120, 256 chunks: 1120 -> 674
+//   80 blocks (3), 16 chunks: 87 -> 103, 32 chunks: 157 -> 149, 256 chunks: 1158 -> 874
+//   128 blocks (2), 32 chunks: 165 -> 173, 64 chunks: 324 -> 315, 256 chunks: 1274 -> 1127
 inline int delta_segments(int64_t blocks, int64_t nc)
 {
-    if (blocks < 1 || blocks > 64 || nc < 32)
+    const int64_t most = blocks < 1 ? 0 : 256 / blocks;
+    if (most < 2 || nc < (most >= 4 ? 16 : (most == 3 ? 32 : 64)))
         return 1;
-    int64_t s = 4;
-    while ((s + 1) * (s + 1) <= nc && s + 1 <= 256 / blocks)
+    int64_t s = most < 4 ? most : 4;
+    while (s < most && (s + 1) * (s + 1) <= 2 * nc)
         ++s;
     const int64_t each = (nc + s - 1) / s;
     return (int)((nc + each - 1) / each);

@@ -308,9 +308,10 @@ template <bool BF, int DKP> struct ScanLds<BF, DKP, true> {  // (no outputs: no 
 
 //
 // With segments (a.nseg > 1) a block walks one of them, from its state in
-// a.start.  STATES: what those are made of, a segment's state from zeros in the
-// blocks of the values' columns, and in the blocks behind them its transition:
-// the columns of the identity, walked without values (r = -X diag(e^G) K S0).
+// a.start.  STATES: what those are made of, a segment's state from zeros (the
+// first one's from state_in) in the blocks of the values' columns, and in the
+// blocks behind them its transition: the columns of the identity, walked without
+// values (r = -X diag(e^G) K S0).
 template <typename D, bool BF, int DKP, int NW, bool VEC, bool STATES>
 __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(BF && STATES ? 2 : 1, BF && STATES ? 2 : 1))) void delta_scan(DeltaArgs a)
 {
@@ -327,10 +328,13 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(BF && S
     const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, col = lane & 15, g = lane >> 4;
     const int vblocks = (a.dvp + 63) / 64, blocks = STATES ? vblocks + DKP / 64 : vblocks;
     uint32_t walk, part;
-    unit_and_part(blockIdx.x, (uint32_t)a.N * a.Hv * a.nseg, blocks, &walk, &part);
-    const int vb = (int)part, seg = (int)(walk % a.nseg);
-    const int64_t head = walk / a.nseg;
+    const int walks = STATES ? a.nseg - 1 : a.nseg;  // (the last one's state and transition are not asked for)
+    unit_and_part(blockIdx.x, (uint32_t)a.N * a.Hv * walks, blocks, &walk, &part);
+    const int vb = (int)part, seg = (int)(walk % walks);
+    const int64_t head = walk / walks;
     const bool values = !STATES || vb < vblocks;
+    if (!values && seg == 0)  // (the first one's state is taken from state_in, not from zeros)
+        return;
     const int n = (int)(head / a.Hv), hv = (int)(head - (int64_t)n * a.Hv), hk = hv / (a.Hv / a.Hk);
     const int v0 = vb * 64, vl = M::at(wave, col >> 2) + (col & 3), v = v0 + vl, cols = min(64, a.Dv - v0);
     const bool mine = v < a.Dv;         // a column of the tensors
@@ -343,9 +347,9 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(BF && S
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
             const int d = M::at(t, g) + r;
-            if (STATES)
+            if (STATES && seg > 0)
                 S[t][r] = !values && d == v - vblocks * 64 ? 1.0f : 0.0f;
-            else if (a.nseg > 1)
+            else if (!STATES && a.nseg > 1)
                 S[t][r] = a.start[((head * a.nseg + seg) * DKP + d) * (vblocks * 64) + v];
             else
                 S[t][r] = a.state_in && mine && d < a.Dk ? a.state_in[(head * a.Dk + d) * a.Dv + v] : 0.0f;
@@ -595,83 +599,75 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(BF && S
             }
 }
 
-// The states before the segments of a head, in order: S <- T S + local, in float.
-// A wave has 16 columns, as in the scan; T comes through LDS, the next segment's
-// in four parts while this one's is multiplied with.  A chain too: 6 us a segment
-// (16 heads, 128 x 128, 8 segments: 49 us).
+// The states before the segments of a head, in order: S <- T S + local, in float,
+// from the first segment's own state.  A block has 16 columns, a wave of it a
+// quarter of the rows: it reads its rows of the next segment's T while it multiplies
+// this one's, and the waves exchange their rows of S through LDS.  A chain of
+// latencies, 4 us a segment (16 heads, 128 x 128, 8 segments: 29 us; 49 with all
+// rows in one wave and T through LDS).
 template <int DKP> __global__ __launch_bounds__(256) void delta_join(DeltaArgs a)
 {
     using M = Mat<false>;
-    constexpr int TK = DKP / 16, PARTS = 4, NL = DKP * DKP / 4 / 256 / PARTS;
-    __shared__ Tile<float, DKP, DKP> s[2];
-    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, g = lane >> 4;
-    const int vblocks = (a.dvp + 63) / 64, width = vblocks * 64 + DKP;
-    const int64_t head = blockIdx.x / vblocks;
-    const int v = (int)(blockIdx.x % vblocks) * 64 + 16 * wave + (lane & 15);
-    f32x4 S[TK], part[NL];
-    const auto load = [&](int seg, int p) {
-        const float* T = a.local + (head * a.nseg + seg) * DKP * width + vblocks * 64;
+    constexpr int TK = DKP / 16, TW = TK / 4;
+    __shared__ f32x4 s[2][TK][64];  // (a tile of S as the lanes have it)
+    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, col = lane & 15, g = lane >> 4, t0 = wave * TW;
+    const int vcols = (a.dvp + 63) / 64 * 64, width = vcols + DKP;
+    const int64_t head = blockIdx.x / (vcols / 16);
+    const int v = (int)(blockIdx.x % (vcols / 16)) * 16 + col;
+    const float* local = a.local + head * a.nseg * DKP * width;
+    float* start = a.start + head * a.nseg * DKP * vcols;
+    f32x4 S[TW], T[TW][TK], own[TW];
+    const auto load = [&](int seg) {
+        const float* from = local + (int64_t)seg * DKP * width;
 #pragma unroll
-        for (int n = 0; n < NL; ++n) {
-            const int i = ((p * NL + n) * 256 + tid) * 4;
-            part[n] = *(const f32x4*)(T + (i / DKP) * width + i % DKP);
+        for (int t = 0; t < TW; ++t) {
+#pragma unroll
+            for (int u = 0; u < TK; ++u)
+                T[t][u] = *(const f32x4*)(from + (16 * (t0 + t) + col) * width + vcols + 16 * u + 4 * g);
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                own[t][r] = from[(M::at(t0 + t, g) + r) * width + v];
         }
     };
-    const auto store = [&](int buf, int p) {
+    load(1);
+    // (the first segment's from here too: state_out may be the array of state_in, and is written by another block)
 #pragma unroll
-        for (int n = 0; n < NL; ++n) {
-            const int i = ((p * NL + n) * 256 + tid) * 4;
-            *(f32x4*)(s[buf].e + s[buf].off(i / DKP, i % DKP)) = part[n];
-        }
-    };
-#pragma unroll
-    for (int p = 0; p < PARTS; ++p) {
-        load(0, p);
-        store(0, p);
-    }
-#pragma unroll
-    for (int t = 0; t < TK; ++t)
+    for (int t = 0; t < TW; ++t)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-            const int d = M::at(t, g) + r;
-            S[t][r] = a.state_in && v < a.Dv && d < a.Dk ? a.state_in[(head * a.Dk + d) * a.Dv + v] : 0.0f;
+            const int d = M::at(t0 + t, g) + r;
+            start[d * vcols + v] = a.state_in && v < a.Dv && d < a.Dk ? a.state_in[(head * a.Dk + d) * a.Dv + v] : 0.0f;
+            S[t][r] = local[d * width + v];
         }
-    for (int seg = 0; seg < a.nseg; ++seg) {
-        float* start = a.start + (head * a.nseg + seg) * DKP * (vblocks * 64) + v;
-        const float* local = a.local + (head * a.nseg + seg) * DKP * width + v;
+    for (int seg = 1; seg < a.nseg; ++seg) {
+        start += DKP * vcols;
 #pragma unroll
-        for (int t = 0; t < TK; ++t)
+        for (int t = 0; t < TW; ++t)
 #pragma unroll
             for (int r = 0; r < 4; ++r)
-                start[(M::at(t, g) + r) * (vblocks * 64)] = S[t][r];
+                start[(M::at(t0 + t, g) + r) * vcols + v] = S[t][r];
         if (seg + 1 == a.nseg)
             break;
+#pragma unroll
+        for (int t = 0; t < TW; ++t)
+            s[seg & 1][t0 + t][lane] = S[t];
         __syncthreads();
-        f32x4 next[TK], own[TK];
+        f32x4 now[TW][TK];
 #pragma unroll
-        for (int t = 0; t < TK; ++t) {
-            next[t] = f32x4{0, 0, 0, 0};
+        for (int t = 0; t < TW; ++t) {
+            S[t] = own[t];
 #pragma unroll
-            for (int r = 0; r < 4; ++r)
-                own[t][r] = local[(M::at(t, g) + r) * width];
+            for (int u = 0; u < TK; ++u)
+                now[t][u] = T[t][u];
         }
+        load(seg + 1);  // (the last segment's: within the array, and not used)
 #pragma unroll
-        for (int p = 0; p < PARTS; ++p) {
-            if (seg + 2 < a.nseg)
-                load(seg + 1, p);
+        for (int u = 0; u < TK; ++u) {
+            const f32x4 b = s[seg & 1][u][lane];
 #pragma unroll
-            for (int u = p * TK / PARTS; u < (p + 1) * TK / PARTS; ++u) {
-                const f32x4 b = M::pack(S + u);
-#pragma unroll
-                for (int t = 0; t < TK; ++t)
-                    next[t] = M::mma(M::rows(s[seg & 1], t, u, tid), b, next[t]);
-            }
-            if (seg + 2 < a.nseg)
-                store((seg + 1) & 1, p);
+            for (int t = 0; t < TW; ++t)
+                S[t] = M::mma(now[t][u], b, S[t]);
         }
-#pragma unroll
-        for (int t = 0; t < TK; ++t)
-            S[t] = next[t] + own[t];
     }
 }
 
@@ -1263,11 +1259,11 @@ template <typename D, bool BF, int DKP, bool VEC> hipError_t forward(const Delta
     const dim3 threads(kScanWaves * 64);
     if (a.nseg > 1) {
         delta_scan<D, BF, DKP, kScanWaves, VEC, true>
-            <<<dim3((unsigned)(heads * a.nseg * (vblocks + DKP / 64))), threads, 0, s>>>(a);
+            <<<dim3((unsigned)(heads * (a.nseg - 1) * (vblocks + DKP / 64))), threads, 0, s>>>(a);
         hipError_t err = hipGetLastError();
         if (err != hipSuccess)
             return err;
-        delta_join<DKP><<<dim3((unsigned)(heads * vblocks)), dim3(256), 0, s>>>(a);
+        delta_join<DKP><<<dim3((unsigned)(heads * vblocks * 4)), dim3(256), 0, s>>>(a);
         if ((err = hipGetLastError()) != hipSuccess)
             return err;
     }

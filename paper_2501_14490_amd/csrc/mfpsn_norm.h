@@ -30,18 +30,21 @@ struct NormArgs {
 // the weights' reads and their join, as long as the loads in flight last: wider
 // rows and tiles have more of them a block.  Measured (us; 1024, 512, 256 blocks):
 //   rows    f32 [500000][64]    75, 82 (512), 77;    f32 [64000][512]   82, 75, 88
-//           bf16 [20000][2048]  95, 72, 62
+//   rows of four waves, one a block  bf16 [20000][2047]  61, -, 124;
+//           bf16 [10000][4096]  74, 58, 80;                bf16 [5000][8191]  154, 117, 99
 //   planes  bf16 [3000][12][1936]  121, 141, -;      bf16 [960][64][1936] 171, 155, 157
 //           bf16 [500][256][700]   155, 136, 161;    bf16 [16][1024][4096] 137, 132, 124
-//   one element a lane and load (rows or planes of odd sizes): twice as many,
-//           bf16 [4811][1001]  18, 20, -;            bf16 [960][64][1935]  191, 214, 217
+//   planes of one column a lane (S odd): twice as many, bf16 [960][64][1935]  191, 214, 217
 constexpr int kNormMaxBlocks = 1024;
 inline int norm_blocks(int64_t M, int64_t C, int64_t S)
 {
     const int64_t work = S == 1 ? (M + 3) / 4 : (M * S + 63) / 64;
-    const int64_t few = S == 1 ? 64 : 16, some = S == 1 ? 1024 : 256;
-    int64_t most = C <= few ? kNormMaxBlocks : (C <= some ? kNormMaxBlocks / 2 : kNormMaxBlocks / 4);
-    if ((S == 1 ? C % 4 : S % 2) && most < kNormMaxBlocks)
+    int64_t most = kNormMaxBlocks;
+    if (S == 1)
+        most = C <= 64 || (C > 1024 && C <= 2048) ? most : (C <= 4096 ? most / 2 : most / 4);
+    else
+        most = C <= 16 ? most : (C <= 256 ? most / 2 : most / 4);
+    if (S > 1 && S % 2 && most < kNormMaxBlocks)
         most *= 2;
     return (int)(work < 1 ? 1 : (work < most ? work : most));
 }

@@ -103,6 +103,26 @@ __device__ __forceinline__ float row_sum(float v, float (*lds)[4], int& at)
     return v;
 }
 
+// N neighbouring elements at any element's address: one read or write of 16 bytes
+// (global memory takes them unaligned; lines that two lanes share are the cost)
+typedef uint32_t WordsAt2 __attribute__((ext_vector_type(4), aligned(2)));
+typedef uint32_t WordsAt4 __attribute__((ext_vector_type(4), aligned(4)));
+template <typename T> struct AnyWords;
+template <> struct AnyWords<uint16_t> { using type = WordsAt2; };
+template <> struct AnyWords<float> { using type = WordsAt4; };
+template <int N, typename T> __device__ __forceinline__ Vec<T, N> read_any(const T* p)
+{
+    using Words = typename AnyWords<T>::type;
+    static_assert(sizeof(T) * N == 16);
+    return __builtin_bit_cast(Vec<T, N>, *(const Words*)p);
+}
+template <typename T, int N> __device__ __forceinline__ void write_any(T* p, const Vec<T, N>& v)
+{
+    using Words = typename AnyWords<T>::type;
+    static_assert(sizeof(T) * N == 16);
+    *(Words*)p = __builtin_bit_cast(Words, v);
+}
+
 // A thread's weights w[at0 + i step + j] (behind C: any), `none` where there are none
 template <int VE, int NV>
 __device__ __forceinline__ void load_weights(const float* __restrict__ w, float none, int at0, int step, int C,
@@ -127,8 +147,46 @@ __device__ __forceinline__ void load_weights(const float* __restrict__ w, float 
 // S = 1
 // ---------------------------------------------------------------------------
 
-// A lane's elements of a row: NV loads of VE neighbours, LANES lanes a row
-template <typename D, int VE, int NV, int LANES>
+// A lane's elements of a row: NV loads of VE neighbours, LANES lanes a row.  ANY:
+// rows that start at no vector's border, of a whole number of vectors or not.  The
+// row's last vector then begins at C - VE: its first elements are the vector's
+// before it, counted there and written twice with the same value.
+template <int VE, bool ANY> struct Row {
+    int e, at, skip;  // the vector's first element, where it is read, elements of it that belong to another
+    __device__ Row(int i, int lanes, int lane, int C)
+    {
+        e = (i * lanes + lane) * VE;
+        at = min(e, C - VE);
+        skip = e - at;
+    }
+    __device__ bool in(int C) const { return e < C; }                       // has elements of the row
+    __device__ bool own(int j, int C) const { return ANY ? j >= skip : e < C; }  // element j is this lane's
+};
+
+// the weights of a lane's vectors; `none` where there are none
+template <int VE, int NV, bool ANY, int LANES>
+__device__ __forceinline__ void row_weights(const float* __restrict__ w, float none, int lane, int C, float (&out)[NV][VE])
+{
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const Row<VE, ANY> row(i, LANES, lane, C);
+        if constexpr (VE >= 4) {
+#pragma unroll
+            for (int j = 0; j < VE; j += 4) {
+                Vec<float, 4> v = {{none, none, none, none}};
+                if (w)
+                    v = read_any<4>(w + row.at + j);
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    out[i][j + k] = v.v[k];
+            }
+        } else {
+            out[i][0] = w ? w[row.at] : none;
+        }
+    }
+}
+
+template <typename D, int VE, int NV, int LANES, bool ANY>
 __global__ __launch_bounds__(kT) void norm_fwd_rows(NormArgs a)
 {
     using T = typename D::T;
@@ -140,8 +198,8 @@ __global__ __launch_bounds__(kT) void norm_fwd_rows(NormArgs a)
     const int C = a.C;
     const float inv = 1.0f / (float)C;
     float gam[NV][VE], bet[NV][VE];
-    load_weights<VE, NV>(a.gamma, 1.0f, lane * VE, LANES * VE, C, gam);
-    load_weights<VE, NV>(a.beta, 0.0f, lane * VE, LANES * VE, C, bet);
+    row_weights<VE, NV, ANY, LANES>(a.gamma, 1.0f, lane, C, gam);
+    row_weights<VE, NV, ANY, LANES>(a.beta, 0.0f, lane, C, bet);
     for (int64_t m = (int64_t)blockIdx.x * ROWS + sub; m < a.M; m += (int64_t)gridDim.x * ROWS) {
         const T* __restrict__ x = (const T*)a.x + m * C;
         T* __restrict__ y = (T*)a.out + m * C;
@@ -150,27 +208,30 @@ __global__ __launch_bounds__(kT) void norm_fwd_rows(NormArgs a)
         float s = 0.0f;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const int e = (i * LANES + lane) * VE;
-            raw[i] = *(const V*)(x + (e < C ? e : 0));
+            const Row<VE, ANY> row(i, LANES, lane, C);
+            if constexpr (ANY)
+                raw[i] = read_any<VE>(x + row.at);
+            else
+                raw[i] = *(const V*)(x + row.at);
         }
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const int e = (i * LANES + lane) * VE;
+            const Row<VE, ANY> row(i, LANES, lane, C);
 #pragma unroll
             for (int j = 0; j < VE; ++j) {
                 f[i][j] = D::get(raw[i].v[j]);
-                s += e < C ? f[i][j] : 0.0f;
+                s += row.own(j, C) ? f[i][j] : 0.0f;
             }
         }
         const float mean = row_sum<LANES>(s, lds, at) * inv;
         float q = 0.0f;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const int e = (i * LANES + lane) * VE;
+            const Row<VE, ANY> row(i, LANES, lane, C);
 #pragma unroll
             for (int j = 0; j < VE; ++j) {
                 f[i][j] -= mean;
-                q += e < C ? f[i][j] * f[i][j] : 0.0f;
+                q += row.own(j, C) ? f[i][j] * f[i][j] : 0.0f;
             }
         }
         const float rstd = 1.0f / sqrtf(row_sum<LANES>(q, lds, at) * inv + a.eps);
@@ -180,13 +241,16 @@ __global__ __launch_bounds__(kT) void norm_fwd_rows(NormArgs a)
         }
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const int e = (i * LANES + lane) * VE;
-            if (e < C) {
+            const Row<VE, ANY> row(i, LANES, lane, C);
+            if (row.in(C)) {
                 V v;
 #pragma unroll
                 for (int j = 0; j < VE; ++j)
                     v.v[j] = D::put(f[i][j] * rstd * gam[i][j] + bet[i][j]);
-                *(V*)(y + e) = v;
+                if constexpr (ANY)
+                    write_any(y + row.at, v);
+                else
+                    *(V*)(y + row.at) = v;
             }
         }
     }
@@ -222,7 +286,7 @@ __global__ __launch_bounds__(kT) void norm_fwd_long(NormArgs a)
     }
 }
 
-template <typename D, int VE, int NV, int LANES>
+template <typename D, int VE, int NV, int LANES, bool ANY>
 __global__ __launch_bounds__(kT) void norm_bwd_rows(NormArgs a)
 {
     using T = typename D::T;
@@ -235,7 +299,7 @@ __global__ __launch_bounds__(kT) void norm_bwd_rows(NormArgs a)
     const int C = a.C;
     const float inv = 1.0f / (float)C;
     float gg[NV][VE] = {}, gb[NV][VE] = {}, gam[NV][VE];
-    load_weights<VE, NV>(a.gamma, 1.0f, lane * VE, LANES * VE, C, gam);
+    row_weights<VE, NV, ANY, LANES>(a.gamma, 1.0f, lane, C, gam);
     for (int64_t m = (int64_t)blockIdx.x * ROWS + sub; m < a.M; m += (int64_t)gridDim.x * ROWS) {
         const T* __restrict__ x = (const T*)a.x + m * C;
         const T* __restrict__ gy = (const T*)a.gy + m * C;
@@ -244,17 +308,23 @@ __global__ __launch_bounds__(kT) void norm_bwd_rows(NormArgs a)
         V vx[NV], vg[NV];
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const int e = (i * LANES + lane) * VE, at = e < C ? e : 0;
-            vx[i] = *(const V*)(x + at);
-            vg[i] = *(const V*)(gy + at);
+            const Row<VE, ANY> row(i, LANES, lane, C);
+            if constexpr (ANY) {
+                vx[i] = read_any<VE>(x + row.at);
+                vg[i] = read_any<VE>(gy + row.at);
+            } else {
+                vx[i] = *(const V*)(x + row.at);
+                vg[i] = *(const V*)(gy + row.at);
+            }
         }
         float sa = 0.0f, sh = 0.0f;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const bool in = (i * LANES + lane) * VE < C;
+            const Row<VE, ANY> row(i, LANES, lane, C);
 #pragma unroll
             for (int j = 0; j < VE; ++j) {
-                const float g = in ? D::get(vg[i].v[j]) : 0.0f, xh = in ? (D::get(vx[i].v[j]) - mean) * rstd : 0.0f;
+                const bool own = row.own(j, C);
+                const float g = own ? D::get(vg[i].v[j]) : 0.0f, xh = own ? (D::get(vx[i].v[j]) - mean) * rstd : 0.0f;
                 gg[i][j] += g * xh;
                 gb[i][j] += g;
                 const float al = g * gam[i][j];
@@ -266,15 +336,18 @@ __global__ __launch_bounds__(kT) void norm_bwd_rows(NormArgs a)
         const float mh = row_sum<LANES>(sh, lds, at) * inv;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const int e = (i * LANES + lane) * VE;
-            if (e < C) {
+            const Row<VE, ANY> row(i, LANES, lane, C);
+            if (row.in(C)) {
                 V v;
 #pragma unroll
                 for (int j = 0; j < VE; ++j) {
                     const float g = D::get(vg[i].v[j]), xh = (D::get(vx[i].v[j]) - mean) * rstd;
                     v.v[j] = D::put(rstd * (g * gam[i][j] - ma - xh * mh));
                 }
-                *(V*)(gx + e) = v;
+                if constexpr (ANY)
+                    write_any(gx + row.at, v);
+                else
+                    *(V*)(gx + row.at) = v;
             }
         }
     }
@@ -298,9 +371,9 @@ __global__ __launch_bounds__(kT) void norm_bwd_rows(NormArgs a)
                         for (int r = 0; r < ROWS - 1; ++r)
                             v += sums[r * LANES + lane];
                 }
-                const int e = (i * LANES + lane) * VE + j;
-                if (sub == 0 && e < C)
-                    part[which * C + e] = v;
+                const Row<VE, ANY> row(i, LANES, lane, C);
+                if (sub == 0 && row.own(j, C))
+                    part[which * C + row.at + j] = v;
             }
 }
 
@@ -674,37 +747,39 @@ __global__ __launch_bounds__(1024) void norm_weights_kernel(const float* __restr
 hipError_t last() { return hipGetLastError(); }
 
 // used: blocks of the launch, `most` or as many as have rows
-template <typename D, int VE, int NV, int LANES>
+template <typename D, int VE, bool ANY, int NV, int LANES>
 hipError_t rows(const NormArgs& a, bool bwd, int most, hipStream_t s, int* used)
 {
     constexpr int ROWS = kT / LANES;
     const int64_t need = (a.M + ROWS - 1) / ROWS;
     *used = need < 1 ? 1 : (int)(need < most ? need : most);
     if (bwd)
-        norm_bwd_rows<D, VE, NV, LANES><<<dim3(*used), dim3(kT), 0, s>>>(a);
+        norm_bwd_rows<D, VE, NV, LANES, ANY><<<dim3(*used), dim3(kT), 0, s>>>(a);
     else
-        norm_fwd_rows<D, VE, NV, LANES><<<dim3(*used), dim3(kT), 0, s>>>(a);
+        norm_fwd_rows<D, VE, NV, LANES, ANY><<<dim3(*used), dim3(kT), 0, s>>>(a);
     return last();
 }
 
-// the smallest of the kernels whose registers hold a row: a part of a wave or
-// a whole one of up to 32 elements a lane, else four waves; false: none does.
-// (f32 [500000][64]: 46 us by quarters of a wave, 96 by waves of 48 idle lanes)
-template <typename D, int VE>
+// the smallest of the kernels whose registers hold a row: a part of a wave, a
+// whole one up to 16 elements a lane (the backward keeps five numbers of each), else
+// four waves up to 32; false: none does.  (f32 [500000][64]: 46 us by quarters of a
+// wave, 96 by waves of 48 idle lanes; bf16 [20000][2047], forward and backward: 32
+// and 61 by four waves of 8 elements a lane, 35 and 92 by one of 32)
+template <typename D, int VE, bool ANY>
 bool launch_rows(const NormArgs& a, bool bwd, int most, hipStream_t s, int* used, hipError_t* err)
 {
     const int64_t per = ((int64_t)a.C + VE - 1) / VE;  // loads of a row
-    constexpr int MAX = 32 / VE < 8 ? 32 / VE : 8;
     const auto fits = [&](int nv, int lanes) { return per <= (int64_t)nv * lanes; };
-    if (fits(1, 8)) *err = rows<D, VE, 1, 8>(a, bwd, most, s, used);
-    else if (fits(1, 16)) *err = rows<D, VE, 1, 16>(a, bwd, most, s, used);
-    else if (fits(1, 32)) *err = rows<D, VE, 1, 32>(a, bwd, most, s, used);
-    else if (fits(1, 64)) *err = rows<D, VE, 1, 64>(a, bwd, most, s, used);
-    else if (fits(2, 64)) *err = rows<D, VE, 2, 64>(a, bwd, most, s, used);
-    else if (fits(4, 64)) *err = rows<D, VE, 4, 64>(a, bwd, most, s, used);
-    else if (MAX == 8 && fits(8, 64)) *err = rows<D, VE, MAX, 64>(a, bwd, most, s, used);
-    else if (fits(4, kT)) *err = rows<D, VE, 4, kT>(a, bwd, most, s, used);
-    else if (MAX == 8 && fits(8, kT)) *err = rows<D, VE, MAX, kT>(a, bwd, most, s, used);
+    if (fits(1, 8)) *err = rows<D, VE, ANY, 1, 8>(a, bwd, most, s, used);
+    else if (fits(1, 16)) *err = rows<D, VE, ANY, 1, 16>(a, bwd, most, s, used);
+    else if (fits(1, 32)) *err = rows<D, VE, ANY, 1, 32>(a, bwd, most, s, used);
+    else if (fits(1, 64)) *err = rows<D, VE, ANY, 1, 64>(a, bwd, most, s, used);
+    else if (fits(2, 64)) *err = rows<D, VE, ANY, 2, 64>(a, bwd, most, s, used);
+    else if (VE == 4 && fits(4, 64)) *err = rows<D, VE, ANY, 4, 64>(a, bwd, most, s, used);
+    else if (VE == 8 && fits(1, kT)) *err = rows<D, VE, ANY, 1, kT>(a, bwd, most, s, used);
+    else if (fits(2, kT)) *err = rows<D, VE, ANY, 2, kT>(a, bwd, most, s, used);
+    else if (fits(4, kT)) *err = rows<D, VE, ANY, 4, kT>(a, bwd, most, s, used);
+    else if (VE == 4 && fits(8, kT)) *err = rows<D, VE, ANY, 8, kT>(a, bwd, most, s, used);
     else return false;
     return true;
 }
@@ -757,9 +832,10 @@ template <typename D, int VE> hipError_t launch_planes(const NormArgs& a, bool b
 // Most blocks of the forward.  A block reads its lanes' weights once, so a few
 // rows each pay for them; fewer blocks leave loads in flight unused.  (us; 2048,
 // 1024, 512, 256 blocks) f32 [64000][512]: 46, 44, 50, 84; f32 [500000][64]: 46,
-// 45, 70, 121; bf16 [20000][2048]: 69, 46, 41, 47.  Tiles: (2048, 4096, 8192,
-// 16384) bf16 [960][64][1936]: 114, 105, 106, 106; bf16 [500][256][700]: 95, 91,
-// 113, 113; one column a lane, bf16 [960][64][1935]: 130, 139, 125, 113.
+// 45, 70, 121; of four waves a row, bf16 [20000][2048]: 29, -, 62, -; bf16
+// [10000][4096]: 34, 32, 51, -.  Tiles: (2048, 4096, 8192, 16384) bf16
+// [960][64][1936]: 114, 105, 106, 106; bf16 [500][256][700]: 95, 91, 113, 113; one
+// column a lane, bf16 [960][64][1935]: 130, 139, 125, 113.
 constexpr int kFwdRows = 1024, kFwdPlanes = 4096;
 
 template <typename D> hipError_t run(const NormArgs& a, bool bwd, hipStream_t s)
@@ -773,9 +849,13 @@ template <typename D> hipError_t run(const NormArgs& a, bool bwd, hipStream_t s)
     int used = blocks;
     hipError_t err = hipSuccess;
     if (a.S == 1) {
-        const int most = bwd ? blocks : (a.C <= 1024 ? kFwdRows : kFwdRows / 2);
-        const bool done = a.C % VE == 0 && al(16) ? launch_rows<D, VE>(a, bwd, most, s, &used, &err)
-                                                  : launch_rows<D, 1>(a, bwd, most, s, &used, &err);
+        const int most = bwd ? blocks : (a.C > 1024 && a.C <= 2048 ? 2 * kFwdRows : kFwdRows);
+        bool done = true;
+        if (a.C < VE)  // (no whole vector)
+            err = rows<D, 1, false, 1, 8>(a, bwd, most, s, &used);
+        else
+            done = a.C % VE == 0 && al(16) ? launch_rows<D, VE, false>(a, bwd, most, s, &used, &err)
+                                           : launch_rows<D, VE, true>(a, bwd, most, s, &used, &err);
         if (!done) {
             whole = false;
             const int g = (int)(a.M < 1 ? 1 : (a.M < (1 << 20) ? a.M : (1 << 20)));

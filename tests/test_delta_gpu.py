@@ -131,7 +131,9 @@ def test_long_sequence_and_slow_decay(dtype):
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("T,N,Hk,Hv,Dk,Dv,lengths", [(4200, 1, 1, 1, 16, 24, None), (5000, 3, 1, 2, 20, 70, [5000, 130, 0]),
                                                      (4161, 1, 1, 2, 128, 16, None), (2049, 2, 2, 2, 40, 33, [2049, 700]),
-                                                     (1985, 4, 8, 8, 16, 70, None)])
+                                                     (1985, 4, 8, 8, 16, 70, None), (1024, 1, 1, 1, 128, 128, None),
+                                                     (2048, 5, 4, 8, 16, 70, [2048, 5, 2047, 900, 0]),
+                                                     (4100, 3, 16, 16, 16, 70, None)])
 def test_segments_of_a_long_sequence(T, N, Hk, Hv, Dk, Dv, lengths, dtype):
     c = make(T, N, Hk, Hv, Dk, Dv, dtype, seed=T, lengths=lengths, rate=0.003)
     if lengths:
@@ -144,6 +146,13 @@ def test_segments_of_a_long_sequence(T, N, Hk, Hv, Dk, Dv, lengths, dtype):
     assert mfpsn.mfpsn_delta_workspace_size(desc) > mfpsn.mfpsn_delta_workspace_size(plain) / 1000 * N
     near(o, o64, BOUND[dtype]["o"], "o")
     near(S, S64, BOUND[dtype]["state"], "state")
+    # the state behind the sequences in the array of the one before them
+    state, again = dev(c["state"]).clone(), torch.empty_like(o)
+    work = torch.empty(mfpsn.mfpsn_delta_workspace_size(desc), dtype=torch.uint8, device=DEV)
+    mfpsn.mfpsn_delta_forward(desc, *[dev(c[n]) for n in NAMES], dev(c["lengths"]) if lengths else None, state, again, state,
+                              None, work, None)
+    torch.cuda.synchronize()
+    assert torch.equal(again, o) and torch.equal(state, S)
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
