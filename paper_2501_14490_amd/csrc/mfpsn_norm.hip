@@ -293,7 +293,8 @@ __global__ __launch_bounds__(kT) void norm_bwd_rows(NormArgs a)
     using V = Vec<T, VE>;
     constexpr int ROWS = kT / LANES;
     __shared__ float lds[2][4];
-    __shared__ float sums[ROWS > 1 ? (ROWS - 1) * LANES : 1];
+    constexpr int WL = LANES < 64 ? LANES : 64;  // lanes of a wave with columns of their own
+    __shared__ float sums[ROWS > 1 ? 3 : 1][2 * VE][WL];
     int at = 0;
     const int lane = threadIdx.x % LANES, sub = threadIdx.x / LANES;
     const int C = a.C;
@@ -354,27 +355,42 @@ __global__ __launch_bounds__(kT) void norm_bwd_rows(NormArgs a)
     if (!a.part)
         return;
     float* __restrict__ part = a.part + (int64_t)blockIdx.x * 2 * C;
+    const int wave = threadIdx.x >> 6;
 #pragma unroll
-    for (int i = 0; i < NV; ++i)
+    for (int i = 0; i < NV; ++i) {
+        float v[2 * VE];
+#pragma unroll
+        for (int j = 0; j < VE; ++j) {
+            v[j] = gg[i][j];
+            v[VE + j] = gb[i][j];
+        }
+        // over the rows of a wave, then the waves
+        if constexpr (ROWS > 1) {
+#pragma unroll
+            for (int o = LANES; o < 64; o <<= 1)
+#pragma unroll
+                for (int j = 0; j < 2 * VE; ++j)
+                    v[j] += __shfl_xor(v[j], o);
+            const bool store = wave > 0 && (int)(threadIdx.x & 63) < WL;
+            __syncthreads();
+#pragma unroll
+            for (int j = 0; j < 2 * VE; ++j)
+                if (store)
+                    sums[wave - 1][j][lane] = v[j];
+            __syncthreads();
+            if (sub == 0)
+#pragma unroll
+                for (int j = 0; j < 2 * VE; ++j)
+                    v[j] = (v[j] + sums[0][j][lane]) + (sums[1][j][lane] + sums[2][j][lane]);
+        }
+        const Row<VE, ANY> row(i, LANES, lane, C);
 #pragma unroll
         for (int j = 0; j < VE; ++j)
-#pragma unroll
-            for (int which = 0; which < 2; ++which) {
-                float v = which ? gb[i][j] : gg[i][j];
-                if constexpr (ROWS > 1) {
-                    __syncthreads();
-                    if (sub > 0)
-                        sums[(sub - 1) * LANES + lane] = v;
-                    __syncthreads();
-                    if (sub == 0)
-#pragma unroll
-                        for (int r = 0; r < ROWS - 1; ++r)
-                            v += sums[r * LANES + lane];
-                }
-                const Row<VE, ANY> row(i, LANES, lane, C);
-                if (sub == 0 && row.own(j, C))
-                    part[which * C + row.at + j] = v;
+            if (sub == 0 && row.own(j, C)) {
+                part[row.at + j] = v[j];
+                part[C + row.at + j] = v[VE + j];
             }
+    }
 }
 
 // rows longer than the registers of a block hold: grad_x here (each input read
