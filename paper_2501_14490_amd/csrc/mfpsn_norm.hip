@@ -10,7 +10,7 @@
 //
 // Both passes are HBM-bound (one read of each input, one write of each output;
 // about 10 flops an element): a copy of 1 GiB reaches 5.1 TB/s.  f32 [64000][512]
-// forward 46 us (5.7 TB/s) and backward 79 (5.0) and 5 for the weights' join; bf16
+// forward 45 us (5.8 TB/s) and backward 77 (5.1) and 5 for the weights' join; bf16
 // [960][64][1936] 94 (5.0) and 168 (4.2) and 5, behind the copy because lines at
 // the tiles' borders are fetched twice; bf16 [16][1024][4096] forward 67 (4.0).
 // A row's values are loaded once and stay in

@@ -680,7 +680,8 @@ def layer_norm_forward(x, gamma=None, beta=None, eps: float = 1e-5, axis: int = 
         if want_stats:
             shape = list(x.shape)
             del shape[axis % x.dim()]
-            mean, rstd = (torch.empty(shape, dtype=torch.float32, device=dev) for _ in range(2))
+            mean = torch.empty(torch.Size(shape), dtype=torch.float32, device=dev)
+            rstd = torch.empty_like(mean)
         mfpsn_layer_norm_forward(M, C, S, dt, x, gamma, beta, eps, y, mean, rstd, stream)
     return (y, mean, rstd) if want_stats else y
 
@@ -706,7 +707,8 @@ def layer_norm_backward(x, gamma, mean, rstd, grad_y, axis: int = 2, want_weight
         if not want_weights:
             mfpsn_layer_norm_backward(M, C, S, dt, x, gamma, mean, rstd, grad_y, grad_x, None, None, None, stream)
             return grad_x
-        grad_gamma, grad_beta = (torch.empty((C,), dtype=torch.float32, device=dev) for _ in range(2))
+        grad_gamma = torch.empty(C, dtype=torch.float32, device=dev)
+        grad_beta = torch.empty_like(grad_gamma)
         need = mfpsn_layer_norm_workspace_size(M, C, S)
         if workspace is None or _nbytes(workspace) < need:
             workspace = torch.empty(max(need, 8), dtype=torch.uint8, device=dev)
@@ -861,8 +863,8 @@ def delta_step(desc: MfpsnDeltaDesc, q, k, v, g, beta, state, out=None, stream=N
     guard, stream = _on(dev, stream)
     with guard:
         if out is None:
-            o = torch.empty((1, desc.N, desc.Hv, desc.Dv), dtype=v.dtype, device=dev)
-            new = torch.empty((desc.N, desc.Hv, desc.Dk, desc.Dv), dtype=torch.float32, device=dev)
+            o = torch.empty(1, desc.N, desc.Hv, desc.Dv, dtype=v.dtype, device=dev)
+            new = torch.empty(desc.N, desc.Hv, desc.Dk, desc.Dv, dtype=torch.float32, device=dev)
         else:
             o, new = out
             _shaped(o, v.dtype, dev, (1, desc.N, desc.Hv, desc.Dv), "o")
