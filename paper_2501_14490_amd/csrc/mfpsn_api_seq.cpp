@@ -69,6 +69,22 @@ size_t segment_bytes(const mfpsn_delta_desc* d, size_t* local)
                                ((int64_t)d->T + kDeltaChunk - 1) / kDeltaChunk, (size_t)delta_dkp(d->Dk), local);
 }
 
+// What the forward keeps for the backward, and behind it its segments' states
+size_t saved_bytes_of(const mfpsn_delta_desc* d)
+{
+    size_t local;
+    return layout_of(d).saved_bytes() + segment_bytes(d, &local);
+}
+
+// The backward's: the gradients of the states behind the chunks, and its segments'
+// own (one like the forward's start, one more)
+size_t grad_bytes_of(const mfpsn_delta_desc* d)
+{
+    size_t local;
+    const size_t all = segment_bytes(d, &local);
+    return layout_of(d).grad_bytes() + 2 * (all - local);
+}
+
 bool by_steps(const mfpsn_delta_desc* d) { return d->T <= kDeltaStepsMaxT; }
 
 // rows that may be read 16 bytes at a time: the base and every row and head
@@ -111,6 +127,15 @@ void fill(DeltaArgs& a, const mfpsn_delta_desc* d, const void* q, const void* k,
     a.g = g;
     a.beta = beta;
     a.lengths = lengths;
+    a.nseg = 1;
+    a.seg_chunks = a.nc;
+}
+
+// The segments of the chunks
+void cut(DeltaArgs& a)
+{
+    a.nseg = delta_segments((int64_t)a.N * a.Hv * ((a.dvp + 63) / 64), a.nc);
+    a.seg_chunks = (a.nc + a.nseg - 1) / a.nseg;
 }
 
 // The arrays of the forward's chunks in `base`
@@ -247,7 +272,7 @@ int mfpsn_delta_saved_size(const mfpsn_delta_desc* desc, size_t* bytes)
         return st;
     if (!bytes)
         return MFPSN_ERR_NULL;
-    *bytes = layout_of(desc).saved_bytes();
+    *bytes = saved_bytes_of(desc);
     return MFPSN_OK;
 }
 
@@ -258,7 +283,7 @@ int mfpsn_delta_backward_workspace_size(const mfpsn_delta_desc* desc, size_t* by
         return st;
     if (!bytes)
         return MFPSN_ERR_NULL;
-    *bytes = layout_of(desc).grad_bytes();
+    *bytes = grad_bytes_of(desc);
     return MFPSN_OK;
 }
 
@@ -283,8 +308,8 @@ int mfpsn_delta_forward(const mfpsn_delta_desc* desc, const void* q, const void*
     const DeltaLayout l = layout_of(desc);
     const bool steps = !saved && by_steps(desc);
     size_t local = 0;
-    const size_t segments = saved || steps ? 0 : segment_bytes(desc, &local);
-    if (saved ? (saved_bytes < l.saved_bytes() || !aligned(saved, 16))
+    const size_t segments = steps ? 0 : segment_bytes(desc, &local);
+    if (saved ? (saved_bytes < saved_bytes_of(desc) || !aligned(saved, 16))
               : (!steps && (!workspace || workspace_bytes < l.chunk_bytes() + segments || !aligned(workspace, 16))))
         return MFPSN_ERR_WORKSPACE;
     DeltaArgs a;
@@ -296,13 +321,10 @@ int mfpsn_delta_forward(const mfpsn_delta_desc* desc, const void* q, const void*
     a.vec_v = wide_rows(v, a.v_row, desc->Dv, es) && wide_rows(o, (int64_t)desc->Hv * desc->Dv, desc->Dv, es);
     if (!steps)
         place(a, l, saved ? saved : workspace, saved != nullptr);
-    a.nseg = 1;
-    a.seg_chunks = a.nc;
     if (segments > 0) {
-        a.nseg = delta_segments((int64_t)a.N * a.Hv * ((a.dvp + 63) / 64), a.nc);
-        a.seg_chunks = (a.nc + a.nseg - 1) / a.nseg;
-        a.local = (float*)((char*)workspace + l.chunk_bytes());
-        a.start = (float*)((char*)workspace + l.chunk_bytes() + local);
+        cut(a);
+        a.local = (float*)(saved ? (char*)saved + l.saved_bytes() : (char*)workspace + l.chunk_bytes());
+        a.start = a.local + local / sizeof(float);
     }
     const hipStream_t s = (hipStream_t)stream;
     return (steps ? launch_delta_steps(a, desc->dtype, s) : launch_delta_forward(a, desc->dtype, s)) == hipSuccess
@@ -334,8 +356,8 @@ int mfpsn_delta_backward(const mfpsn_delta_desc* desc, const void* q, const void
         !aligned(grad_state_in, 4))
         return MFPSN_ERR_ALIGN;
     const DeltaLayout l = layout_of(desc);
-    if (desc->T > 0 && (!saved || saved_bytes < l.saved_bytes() || !aligned(saved, 16) || !workspace ||
-                        workspace_bytes < l.grad_bytes() || !aligned(workspace, 16)))
+    if (desc->T > 0 && (!saved || saved_bytes < saved_bytes_of(desc) || !aligned(saved, 16) || !workspace ||
+                        workspace_bytes < grad_bytes_of(desc) || !aligned(workspace, 16)))
         return MFPSN_ERR_WORKSPACE;
     DeltaArgs a;
     fill(a, desc, q, k, v, g, beta, lengths);
@@ -345,6 +367,13 @@ int mfpsn_delta_backward(const mfpsn_delta_desc* desc, const void* q, const void
     a.grad_o = grad_o;
     a.grad_state_out = grad_state_out;
     a.dS = workspace;
+    size_t local;
+    if (const size_t segments = segment_bytes(desc, &local); segments > 0) {
+        cut(a);
+        a.local = (float*)((char*)const_cast<void*>(saved) + l.saved_bytes());
+        a.start = (float*)((char*)workspace + l.grad_bytes());
+        a.local2 = a.start + (segments - local) / sizeof(float);
+    }
     a.grad_q = grad_q;
     a.grad_k = grad_k;
     a.grad_v = grad_v;

@@ -38,7 +38,8 @@ struct DeltaArgs {
     int32_t nseg, seg_chunks;     // 1 and nc where there is one
     float* local;                 // [head][nseg][dkp][64 vblocks + dkp]: a segment's state from zeros, its transition
                                   // (the last: neither; the first: its state from state_in)
-    float* start;                 // [head][nseg][dkp][64 vblocks]: the state before each segment
+    float* start;                 // [head][nseg][dkp][64 vblocks]: the state before each segment (backward: the gradient of it behind)
+    float* local2;                // backward, likewise: the gradient before each segment from zeros behind it
     // backward
     const void* grad_o;
     const float* grad_state_out;  // nullable: zeros
@@ -75,6 +76,10 @@ inline int delta_dkp(int Dk) { return Dk <= 64 ? 64 : 128; }
 //   64 blocks (4), 16 chunks: 85 -> 85, 32 chunks: 151 -> 120, 256 chunks: 1120 -> 674
 //   80 blocks (3), 16 chunks: 87 -> 103, 32 chunks: 157 -> 149, 256 chunks: 1158 -> 874
 //   128 blocks (2), 32 chunks: 165 -> 173, 64 chunks: 324 -> 315, 256 chunks: 1274 -> 1127
+// The backward walks the same segments in reverse, with the forward's transitions
+// transposed (forward that keeps for it, and backward, us): 8 blocks, 64 chunks:
+// 276 -> 108 and 228 -> 97, 64 blocks, 32 chunks: 156 -> 125 and 156 -> 127, 128
+// blocks, 64 chunks: 357 -> 351 and 460 -> 477.
 inline int delta_segments(int64_t blocks, int64_t nc)
 {
     const int64_t most = blocks < 1 ? 0 : 256 / blocks;
@@ -87,7 +92,8 @@ inline int delta_segments(int64_t blocks, int64_t nc)
     return (int)((nc + each - 1) / each);
 }
 
-// Bytes of the segments' states (local, start) of a forward, 0 without segments
+// Bytes of the segments' states (local, start) of a forward, 0 without segments (the
+// backward reads local, and has two arrays like start)
 inline size_t delta_segment_bytes(int64_t heads, int64_t dvp, int64_t nc, size_t dkp, size_t* local)
 {
     const size_t vcols = (size_t)(dvp + 63) / 64 * 64;

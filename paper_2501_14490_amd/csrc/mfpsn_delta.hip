@@ -406,7 +406,7 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(BF && S
             store_rows<M, D, VEC>(s.o, (T*)a.o + ((row0 - (int64_t)L * a.N) * a.Hv + hv) * a.Dv + v0, a.o_step, L, cols,
                                   again(threadIdx.x));
         __syncthreads();
-        if (a.S0 && wide) {  // [v][d], for the backward
+        if (!STATES && a.S0 && wide) {  // [v][d], for the backward
             El* S0 = (El*)a.S0 + (unit * a.dvp + v) * DKP + M::at(0, g);
 #pragma unroll
             for (int u = 0; u < UK; ++u)
@@ -517,7 +517,7 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(BF && S
         in_order();
         read_kt(0);
         in_order();
-        if (a.U && wide) {  // [v][i]
+        if (!STATES && a.U && wide) {  // [v][i]
             El* pu = (El*)a.U + (unit * a.dvp + v) * L + M::at(0, g);
 #pragma unroll
             for (int u = 0; u < UL; ++u)
@@ -671,6 +671,66 @@ template <int DKP> __global__ __launch_bounds__(256) void delta_join(DeltaArgs a
     }
 }
 
+// The gradients of the states behind the segments of a head, in reverse: dS <- T^T dS
+// + local, in the same manner, from the last segment's own
+template <int DKP> __global__ __launch_bounds__(256) void delta_rjoin(DeltaArgs a)
+{
+    using M = Mat<false>;
+    constexpr int TK = DKP / 16, TW = TK / 4;
+    __shared__ f32x4 s[2][TK][64];
+    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, col = lane & 15, g = lane >> 4, t0 = wave * TW;
+    const int vcols = (a.dvp + 63) / 64 * 64, width = vcols + DKP;
+    const int64_t head = blockIdx.x / (vcols / 16);
+    const int v = (int)(blockIdx.x % (vcols / 16)) * 16 + col;
+    const float* trans = a.local + head * a.nseg * DKP * width + vcols;
+    const float* local = a.local2 + head * a.nseg * DKP * vcols;
+    float* start = a.start + head * a.nseg * DKP * vcols;
+    f32x4 S[TW];
+#pragma unroll
+    for (int t = 0; t < TW; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int d = M::at(t0 + t, g) + r;
+            start[((a.nseg - 1) * DKP + d) * vcols + v] =
+                a.grad_state_out && v < a.Dv && d < a.Dk ? a.grad_state_out[(head * a.Dk + d) * a.Dv + v] : 0.0f;
+            S[t][r] = local[((a.nseg - 1) * DKP + d) * vcols + v];
+        }
+    for (int seg = a.nseg - 2; seg >= 0; --seg) {
+#pragma unroll
+        for (int t = 0; t < TW; ++t)
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                start[(seg * DKP + M::at(t0 + t, g) + r) * vcols + v] = S[t][r];
+        if (seg == 0)
+            break;
+        const float* from = trans + (int64_t)seg * DKP * width;
+        f32x4 T[TW][TK];
+#pragma unroll
+        for (int t = 0; t < TW; ++t)
+#pragma unroll
+            for (int u = 0; u < TK; ++u)
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    T[t][u][r] = from[(16 * u + 4 * g + r) * width + 16 * (t0 + t) + col];
+#pragma unroll
+        for (int t = 0; t < TW; ++t)
+            s[seg & 1][t0 + t][lane] = S[t];
+        __syncthreads();
+#pragma unroll
+        for (int t = 0; t < TW; ++t)
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                S[t][r] = local[(seg * DKP + M::at(t0 + t, g) + r) * vcols + v];
+#pragma unroll
+        for (int u = 0; u < TK; ++u) {
+            const f32x4 b = s[seg & 1][u][lane];
+#pragma unroll
+            for (int t = 0; t < TW; ++t)
+                S[t] = M::mma(T[t][u], b, S[t]);
+        }
+    }
+}
+
 // The chunks in reverse, in the same manner: the gradient of the state, the
 // values' gradient.  The state's gradient is held in float; as an operand it is
 // rounded once to 16 bits, like the residuals' gradients: what comes of them is
@@ -687,7 +747,11 @@ template <bool BF, int DKP> struct RscanLds {
     alignas(16) float gate[3 * L];
 };
 
-template <typename D, bool BF, int DKP, int NW, bool VEC>
+//
+// With segments, as in the forward: a block walks one, from the gradient in
+// a.start.  STATES: the gradient before a segment from zeros behind it, from
+// grad_state_out for the last; its transition is the forward's, transposed.
+template <typename D, bool BF, int DKP, int NW, bool VEC, bool STATES>
 __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(1, 1))) void delta_rscan(DeltaArgs a)
 {
     using T = typename D::T;
@@ -700,19 +764,26 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(1, 1)))
     __shared__ Lds s;
     const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, col = lane & 15, g = lane >> 4;
     uint32_t walk, vb;
-    unit_and_part(blockIdx.x, (uint32_t)a.N * a.Hv, (a.dvp + 63) / 64, &walk, &vb);
-    const int64_t head = walk;
+    const int vblocks = (a.dvp + 63) / 64, walks = STATES ? a.nseg - 1 : a.nseg;  // (STATES: all but the first)
+    unit_and_part(blockIdx.x, (uint32_t)a.N * a.Hv * walks, vblocks, &walk, &vb);
+    const int64_t head = walk / walks;
+    const int seg = (int)(walk % walks) + (STATES ? 1 : 0);
     const int n = (int)(head / a.Hv), hv = (int)(head - (int64_t)n * a.Hv), hk = hv / (a.Hv / a.Hk);
     const int v0 = (int)vb * 64, vl = M::at(wave, col >> 2) + (col & 3), v = v0 + vl, cols = min(64, a.Dv - v0);
     const bool mine = v < a.Dv, wide = v < a.dvp;
-    const int len = length_of(a, n), chunks = (len + L - 1) / L;
+    const int len = length_of(a, n), all = (len + L - 1) / L;
+    const int first = min(seg * a.seg_chunks, all), chunks = min(first + a.seg_chunks, all);
+    const bool last_seg = seg == a.nseg - 1;
     f32x4 S[TK];
 #pragma unroll
     for (int t = 0; t < TK; ++t)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
             const int d = M::at(t, g) + r;
-            S[t][r] = a.grad_state_out && mine && d < a.Dk ? a.grad_state_out[(head * a.Dk + d) * a.Dv + v] : 0.0f;
+            if (!STATES && a.nseg > 1)
+                S[t][r] = a.start[((head * a.nseg + seg) * DKP + d) * (vblocks * 64) + v];
+            else
+                S[t][r] = last_seg && a.grad_state_out && mine && d < a.Dk ? a.grad_state_out[(head * a.Dk + d) * a.Dv + v] : 0.0f;
         }
     Rows<D, El, DKP, TH, VEC> nk, nq;
     Rows<D, El, 64, TH, VEC> no;
@@ -734,11 +805,11 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(1, 1)))
             ngate = a.gate[unit * 3 * L + min(tid, 3 * L - 1)];
         }
     };
-    if (chunks > 0)
+    if (first < chunks)
 #pragma unroll
         for (int part = 0; part < 4; ++part)
             fetch(chunks - 1, part, tid);
-    for (int c = chunks - 1; c >= 0; --c) {
+    for (int c = chunks - 1; c >= first; --c) {
         const int t0 = c * L, live = min(L, len - t0);
         const int64_t row0 = (int64_t)t0 * a.N + n, unit = unit_of(a, n, hv, c);
         __syncthreads();
@@ -749,11 +820,11 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(1, 1)))
         if (tid < 3 * L)
             s.gate[tid] = ngate;
         no.store(s.dO, live, cols, tid);
-        if (c + 1 < chunks)  // the chunk behind, whose gradients wait in LDS
+        if (!STATES && c + 1 < chunks)  // the chunk behind, whose gradients wait in LDS
             store_rows<M, D, VEC>(s.dV, (T*)a.grad_v + ((row0 + (int64_t)L * a.N) * a.Hv + hv) * a.Dv + v0, a.o_step,
                                   min(L, len - t0 - L), cols, again(threadIdx.x));
         __syncthreads();
-        if (wide) {  // [v][d], for delta_grads
+        if (!STATES && wide) {  // [v][d], for delta_grads
             El* dS = (El*)a.dS + (unit * a.dvp + v) * DKP + M::at(0, g);
 #pragma unroll
             for (int u = 0; u < UK; ++u)
@@ -774,7 +845,7 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(1, 1)))
         in_order();
 #pragma unroll
         for (int u = 0; u < UK; ++u) {
-            if (c > 0)
+            if (c > first)
 #pragma unroll
                 for (int part = 0; part < 4; ++part)
                     if (part * UK / 4 == u)
@@ -866,9 +937,10 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(1, 1)))
                 if (M::reaches(t, u * TU))
                     dV[t] = M::mma(fx[u][t], b, dV[t]);
         }
+        if (!STATES)
 #pragma unroll
-        for (int u = 0; u < UL; ++u)
-            *(Frag*)(s.dV.e + s.dV.off(vl, u * KU + M::at(0, g))) = M::pack(dV + u * TU);
+            for (int u = 0; u < UL; ++u)
+                *(Frag*)(s.dV.e + s.dV.off(vl, u * KU + M::at(0, g))) = M::pack(dV + u * TU);
 #pragma unroll
         for (int t = 0; t < 4; ++t)
 #pragma unroll
@@ -886,15 +958,26 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(1, 1)))
             in_order();
         }
     }
-    if (chunks > 0) {  // the first chunk's gradients
+    if constexpr (STATES) {
+        float* local = a.local2 + (head * a.nseg + seg) * DKP * (vblocks * 64) + v;
+#pragma unroll
+        for (int t = 0; t < TK; ++t)
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                local[(M::at(t, g) + r) * (vblocks * 64)] = S[t][r];
+        return;
+    }
+    if (first < chunks) {  // the first chunk's gradients
         __syncthreads();
-        store_rows<M, D, VEC>(s.dV, (T*)a.grad_v + ((int64_t)n * a.Hv + hv) * a.Dv + v0, a.o_step, min(L, len), cols, tid);
+        const int64_t row0 = (int64_t)first * L * a.N + n;
+        store_rows<M, D, VEC>(s.dV, (T*)a.grad_v + (row0 * a.Hv + hv) * a.Dv + v0, a.o_step, min(L, len - first * L), cols, tid);
     }
     if (!mine)
         return;
-    for (int t = len + (lane >> 4); t < a.T; t += 4)
-        ((T*)a.grad_v)[(((int64_t)t * a.N + n) * a.Hv + hv) * a.Dv + v] = D::put(0.0f);
-    if (a.grad_state_in)
+    const int64_t end = min((int64_t)a.T, (int64_t)(seg + 1) * a.seg_chunks * L);
+    for (int64_t t = max((int64_t)len, (int64_t)seg * a.seg_chunks * L) + (lane >> 4); t < end; t += 4)
+        ((T*)a.grad_v)[((t * a.N + n) * a.Hv + hv) * a.Dv + v] = D::put(0.0f);
+    if (a.grad_state_in && seg == 0)
 #pragma unroll
         for (int t = 0; t < TK; ++t)
 #pragma unroll
@@ -1245,8 +1328,6 @@ __global__ __launch_bounds__((GradsShape<BF, ONE>::THREADS), 2) void delta_grads
 
 constexpr int kScanWaves = 4;
 
-int64_t scan_blocks(const DeltaArgs& a) { return (int64_t)a.N * a.Hv * ((a.dvp + 16 * kScanWaves - 1) / (16 * kScanWaves)); }
-
 template <typename D, bool BF, int DKP, bool VEC> hipError_t forward(const DeltaArgs& a, hipStream_t s)
 {
     if (a.nc > 0) {
@@ -1273,8 +1354,19 @@ template <typename D, bool BF, int DKP, bool VEC> hipError_t forward(const Delta
 
 template <typename D, bool BF, int DKP, bool VEC> hipError_t backward(const DeltaArgs& a, hipStream_t s)
 {
-    delta_rscan<D, BF, DKP, kScanWaves, VEC><<<dim3((unsigned)scan_blocks(a)), dim3(kScanWaves * 64), 0, s>>>(a);
-    const hipError_t err = hipGetLastError();
+    const int64_t heads = (int64_t)a.N * a.Hv, vblocks = (a.dvp + 63) / 64;
+    const dim3 threads(kScanWaves * 64);
+    hipError_t err;
+    if (a.nseg > 1) {
+        delta_rscan<D, BF, DKP, kScanWaves, VEC, true><<<dim3((unsigned)(heads * (a.nseg - 1) * vblocks)), threads, 0, s>>>(a);
+        if ((err = hipGetLastError()) != hipSuccess)
+            return err;
+        delta_rjoin<DKP><<<dim3((unsigned)(heads * vblocks * 4)), dim3(256), 0, s>>>(a);
+        if ((err = hipGetLastError()) != hipSuccess)
+            return err;
+    }
+    delta_rscan<D, BF, DKP, kScanWaves, VEC, false><<<dim3((unsigned)(heads * a.nseg * vblocks)), threads, 0, s>>>(a);
+    err = hipGetLastError();
     if (err != hipSuccess || a.nc == 0)
         return err;
     const dim3 grid((unsigned)((int64_t)a.N * a.Hk * a.nc));

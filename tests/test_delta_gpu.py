@@ -155,6 +155,19 @@ def test_segments_of_a_long_sequence(T, N, Hk, Hv, Dk, Dv, lengths, dtype):
     assert torch.equal(again, o) and torch.equal(state, S)
 
 
+# the backward of such sequences: the gradients of the states between the segments, joined in reverse
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("T,N,Hk,Hv,Dk,Dv,lengths", [(1100, 1, 1, 2, 64, 70, None), (2049, 3, 1, 2, 20, 40, [2049, 130, 0]),
+                                                     (1500, 2, 2, 2, 128, 128, [1500, 700]), (4100, 1, 1, 1, 16, 16, None)])
+def test_gradients_of_a_long_sequence(T, N, Hk, Hv, Dk, Dv, lengths, dtype):
+    c = make(T, N, Hk, Hv, Dk, Dv, dtype, seed=T, lengths=lengths, rate=0.01)
+    if lengths:
+        for n in range(N):
+            for name in NAMES + ("grad_o",):
+                c[name][lengths[n]:, n] = float("nan")
+    check(c)
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("T,lengths", [(150, [150, 0, 1, 64, 65, 149]), (6, [6, 0, 3, 1, 5, 2]), (70, [0, 0, 0, 0, 0, 0]),
                                        (64, [64, 200, -3, 63, 1, 32])])
