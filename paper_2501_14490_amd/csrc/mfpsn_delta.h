@@ -78,8 +78,8 @@ inline int delta_dkp(int Dk) { return Dk <= 64 ? 64 : 128; }
 //   128 blocks (2), 32 chunks: 165 -> 173, 64 chunks: 324 -> 315, 256 chunks: 1274 -> 1127
 // The backward walks the same segments in reverse, with the forward's transitions
 // transposed (forward that keeps for it, and backward, us): 8 blocks, 64 chunks:
-// 276 -> 108 and 228 -> 97, 64 blocks, 32 chunks: 156 -> 125 and 156 -> 127, 128
-// blocks, 64 chunks: 357 -> 351 and 460 -> 477.
+// 276 -> 108 and 228 -> 86, 64 blocks, 32 chunks: 156 -> 126 and 156 -> 118, 128
+// blocks, 64 chunks: 357 -> 350 and 460 -> 444.
 inline int delta_segments(int64_t blocks, int64_t nc)
 {
     const int64_t most = blocks < 1 ? 0 : 256 / blocks;

@@ -749,9 +749,11 @@ template <bool BF, int DKP> struct RscanLds {
 
 //
 // With segments, as in the forward: a block walks one, from the gradient in
-// a.start.  STATES: the gradient before a segment from zeros behind it, from
+// a.start.  kStates: the gradient before a segment from zeros behind it, from
 // grad_state_out for the last; its transition is the forward's, transposed.
-template <typename D, bool BF, int DKP, int NW, bool VEC, bool STATES>
+// (kWhole is a kernel of its own: one for both took 159 us where it takes 135)
+enum RscanWalk { kWhole, kSegment, kStates };
+template <typename D, bool BF, int DKP, int NW, bool VEC, RscanWalk WALK>
 __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(1, 1))) void delta_rscan(DeltaArgs a)
 {
     using T = typename D::T;
@@ -759,31 +761,33 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(1, 1)))
     using El = typename M::El;
     using Frag = typename M::Frag;
     using Lds = RscanLds<BF, DKP>;
+    constexpr bool STATES = WALK == kStates;
     constexpr int TK = DKP / 16, TH = NW * 64, KU = M::KU, TU = M::TU, UK = DKP / KU, UL = L / KU;
     static_assert(NW == 4 && TH >= 3 * L);
     __shared__ Lds s;
     const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, col = lane & 15, g = lane >> 4;
     uint32_t walk, vb;
-    const int vblocks = (a.dvp + 63) / 64, walks = STATES ? a.nseg - 1 : a.nseg;  // (STATES: all but the first)
+    const int vblocks = (a.dvp + 63) / 64, walks = STATES ? a.nseg - 1 : (WALK == kWhole ? 1 : a.nseg);  // (STATES: all but the first)
     unit_and_part(blockIdx.x, (uint32_t)a.N * a.Hv * walks, vblocks, &walk, &vb);
-    const int64_t head = walk / walks;
-    const int seg = (int)(walk % walks) + (STATES ? 1 : 0);
+    const int64_t head = WALK == kWhole ? walk : walk / walks;
+    const int seg = WALK == kWhole ? 0 : (int)(walk % walks) + (STATES ? 1 : 0);
     const int n = (int)(head / a.Hv), hv = (int)(head - (int64_t)n * a.Hv), hk = hv / (a.Hv / a.Hk);
     const int v0 = (int)vb * 64, vl = M::at(wave, col >> 2) + (col & 3), v = v0 + vl, cols = min(64, a.Dv - v0);
     const bool mine = v < a.Dv, wide = v < a.dvp;
     const int len = length_of(a, n), all = (len + L - 1) / L;
-    const int first = min(seg * a.seg_chunks, all), chunks = min(first + a.seg_chunks, all);
-    const bool last_seg = seg == a.nseg - 1;
+    const int first = WALK == kWhole ? 0 : min(seg * a.seg_chunks, all);
+    const int chunks = WALK == kWhole ? all : min(first + a.seg_chunks, all);
+    const bool from_out = WALK == kWhole || seg == a.nseg - 1;
     f32x4 S[TK];
 #pragma unroll
     for (int t = 0; t < TK; ++t)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
             const int d = M::at(t, g) + r;
-            if (!STATES && a.nseg > 1)
+            if (WALK == kSegment)
                 S[t][r] = a.start[((head * a.nseg + seg) * DKP + d) * (vblocks * 64) + v];
             else
-                S[t][r] = last_seg && a.grad_state_out && mine && d < a.Dk ? a.grad_state_out[(head * a.Dk + d) * a.Dv + v] : 0.0f;
+                S[t][r] = from_out && a.grad_state_out && mine && d < a.Dk ? a.grad_state_out[(head * a.Dk + d) * a.Dv + v] : 0.0f;
         }
     Rows<D, El, DKP, TH, VEC> nk, nq;
     Rows<D, El, 64, TH, VEC> no;
@@ -974,7 +978,7 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(1, 1)))
     }
     if (!mine)
         return;
-    const int64_t end = min((int64_t)a.T, (int64_t)(seg + 1) * a.seg_chunks * L);
+    const int64_t end = WALK == kWhole ? a.T : min((int64_t)a.T, (int64_t)(seg + 1) * a.seg_chunks * L);
     for (int64_t t = max((int64_t)len, (int64_t)seg * a.seg_chunks * L) + (lane >> 4); t < end; t += 4)
         ((T*)a.grad_v)[((t * a.N + n) * a.Hv + hv) * a.Dv + v] = D::put(0.0f);
     if (a.grad_state_in && seg == 0)
@@ -1358,14 +1362,17 @@ template <typename D, bool BF, int DKP, bool VEC> hipError_t backward(const Delt
     const dim3 threads(kScanWaves * 64);
     hipError_t err;
     if (a.nseg > 1) {
-        delta_rscan<D, BF, DKP, kScanWaves, VEC, true><<<dim3((unsigned)(heads * (a.nseg - 1) * vblocks)), threads, 0, s>>>(a);
+        delta_rscan<D, BF, DKP, kScanWaves, VEC, kStates><<<dim3((unsigned)(heads * (a.nseg - 1) * vblocks)), threads, 0, s>>>(a);
         if ((err = hipGetLastError()) != hipSuccess)
             return err;
         delta_rjoin<DKP><<<dim3((unsigned)(heads * vblocks * 4)), dim3(256), 0, s>>>(a);
         if ((err = hipGetLastError()) != hipSuccess)
             return err;
     }
-    delta_rscan<D, BF, DKP, kScanWaves, VEC, false><<<dim3((unsigned)(heads * a.nseg * vblocks)), threads, 0, s>>>(a);
+    if (a.nseg > 1)
+        delta_rscan<D, BF, DKP, kScanWaves, VEC, kSegment><<<dim3((unsigned)(heads * a.nseg * vblocks)), threads, 0, s>>>(a);
+    else
+        delta_rscan<D, BF, DKP, kScanWaves, VEC, kWhole><<<dim3((unsigned)(heads * vblocks)), threads, 0, s>>>(a);
     err = hipGetLastError();
     if (err != hipSuccess || a.nc == 0)
         return err;
